@@ -20,6 +20,10 @@
  * the paper's own grouping (statistics per channel over 32 tokens), with the
  * same Qhat and update matrix.
  *
+ * squat_paged_write / squat_paged_read / squat_paged_attention serve sequences
+ * of different lengths from pages of packed keys and values;
+ * squat_verify_drafts decides on drafted tokens.
+ *
  * Conventions that hold for every call
  *   - Every data pointer is a DEVICE pointer owned by the caller, valid on the
  *     device that is current when the call is made.  Only `ws` buffers are
@@ -593,6 +597,158 @@ int squat_cache_key_scores(const squat_cache* cache, const void* q, squat_dtype 
 int squat_cache_key_scores_rope(const squat_cache* cache, const void* q, squat_dtype q_dt, int64_t q_stride_batch,
                                 int64_t q_stride_head, const float* inv_freq, int64_t pos0, float out_scale,
                                 float* scores, int64_t s_stride_batch, int64_t s_stride_head, squat_stream stream);
+
+/* ------------------------------------------------------------------------- *
+ * squat_paged_*  (decoding phase of Algorithm 1 for sequences of different
+ * lengths; Section 2 "Quantization": qtz/deq; appendix "Details of Our Main
+ * Algorithm" for the values' per-token groups).
+ *
+ * A store of pages: page_tokens tokens of every KV head each, all in packed
+ * codes with one (scale, zero-point) pair per token and group of `group`
+ * channels.  A sequence is a list of pages in any order; token t of it lies in
+ * its page t / page_tokens at offset t mod page_tokens, i.e. in slot
+ *     page * page_tokens + offset.
+ *   codes    [n_pages, n_kv_heads, page_tokens, d*bits/32] uint32, the layout of
+ *            a row as for squat_quantize_keys.
+ *   meta     [n_pages, n_kv_heads, page_tokens, d/group, 2] fp16 bit patterns:
+ *            scale, zero-point.
+ *   All four arrays dense and 16-byte aligned.  bits 2, 4 or 8; group 32, 64 or
+ *   128; page_tokens a power of two from 16 to 1024; 1 <= n_pages < 2^31.
+ * The caller owns the arrays and says which page belongs to whom.
+ * ------------------------------------------------------------------------- */
+typedef struct squat_paged_store {
+    uint32_t* key_codes;
+    uint16_t* key_meta;
+    uint32_t* value_codes;
+    uint16_t* value_meta;
+    int64_t n_pages;
+    int n_kv_heads;
+    int page_tokens;
+    int d;                /* 128 */
+    int bits;
+    int group;
+} squat_paged_store;
+
+/* ------------------------------------------------------------------------- *
+ * squat_paged_write  -- quantizes the keys and values of n_tokens tokens into
+ * their slots.
+ *
+ *   k, v     [n_tokens, n_kv_heads, d] dtype dt, element (t,h,c) at
+ *            k[t*stride_token + h*stride_head + c]; both with these strides
+ *            (multiples of 8 elements), bases 16-byte aligned.
+ *   slots    [n_tokens] int64, device memory.  A slot outside [0, n_pages *
+ *            page_tokens) is skipped: its token goes nowhere (padding).  Two
+ *            tokens with one slot: the slot's contents are undefined.
+ *   update   NULL: keys and values both by plain round-to-nearest, per group
+ *                zero  = fp16(min),   scale = fp16(fp32((max - min) / (2^b - 1))),
+ *                code  = clamp(rint((x - zero) / scale), 0, 2^b - 1)
+ *            where the quotient is decided as in 64 bits (ties to even); scale 0
+ *            gives code 0.  Values must stay below 65504; a NaN or an infinity
+ *            spoils its own group (which then reads as NaN or infinity).
+ *            Otherwise [n_kv_heads, d, d] float as for squat_quantize_keys: the
+ *            keys are what that call writes for `bits` (2 or 4), `group` and g.
+ *   ws       with an update matrix scratch of squat_paged_write_workspace(...)
+ *            bytes, 256-byte aligned; else not looked at.
+ *   n_tokens may be 0 (nothing is launched).
+ * ------------------------------------------------------------------------- */
+size_t squat_paged_write_workspace(const squat_paged_store* store, int64_t n_tokens, int has_update);
+
+int squat_paged_write(const squat_paged_store* store, const void* k, const void* v, squat_dtype dt, int64_t n_tokens,
+                      int64_t stride_token, int64_t stride_head, const int64_t* slots, const float* update, int g,
+                      void* ws, size_t ws_bytes, squat_stream stream);
+
+/* ------------------------------------------------------------------------- *
+ * squat_paged_read  -- what the store holds in n_tokens slots:
+ * code * scale + zero, one fused multiply-add in fp32, rounded once to out_dt.
+ *
+ *   slots    as for squat_paged_write; a slot outside the store reads as zeros.
+ *   k_out, v_out  [n_tokens, n_kv_heads, d] dtype out_dt, strides and alignment
+ *            as for squat_paged_write.  Either may be NULL (not read).
+ * ------------------------------------------------------------------------- */
+int squat_paged_read(const squat_paged_store* store, const int64_t* slots, int64_t n_tokens, void* k_out, void* v_out,
+                     squat_dtype out_dt, int64_t stride_token, int64_t stride_head, squat_stream stream);
+
+/* ------------------------------------------------------------------------- *
+ * squat_paged_attention  -- attention of the new tokens of n_seqs sequences
+ * over everything each of them has in the store, its new tokens included (which
+ * are written first).
+ *
+ * Sequence s has kv_len[s] tokens in the pages pages[s, 0 ..], the last
+ * n = q_start[s+1] - q_start[s] of which are new.  Its i-th new token is at
+ * position P = kv_len[s] - n + i and sees the tokens 0 .. P; for query head hq
+ * and KV head h = hq / q_per_kv
+ *     out[q_start[s] + i, hq, :] = sum_t p_t v_t,
+ *     p = softmax_{t <= P}(out_scale * q . k_t),    lse = log sum_t exp(...)
+ * with k_t, v_t as squat_paged_read gives them (fp32).  A token that sees nothing
+ * (P < 0) gives zeros and lse = -infinity.  A token whose scale or zero-point is
+ * not finite gives NaN to what sees it (a key's to the whole row, a value's to
+ * its group's channels), and to nothing else.
+ *
+ *   q        [n_new, n_kv_heads*q_per_kv, d] dtype q_dt (fp16 or bf16), element
+ *            (t,hq,c) at q[t*q_stride_token + hq*q_stride_head + c]; base 16-byte
+ *            aligned, strides multiples of 8 elements.  q_per_kv 1 .. 16.
+ *   q_start  [n_seqs + 1] int32, device memory, ascending from 0 to n_new; two
+ *            equal entries: a sequence without new tokens.
+ *   kv_len   [n_seqs] int32, device memory; entries beyond the page list's room
+ *            (pages_per_seq * page_tokens) count as that room, negative ones as 0.
+ *   pages    [n_seqs, pages_per_seq] int32, device memory, rows page_stride
+ *            entries apart.  Tokens in a page outside [0, n_pages) are seen by
+ *            nobody.  Entries past a sequence's last token are not looked at.
+ *   max_new, max_kv   the largest number of new tokens and the largest kv_len, or
+ *            0: as large as n_new and the page lists allow.  Hints for the
+ *            launch's shape: results are right for any values, fastest for true ones.
+ *   out      [n_new, n_kv_heads*q_per_kv, d] dtype q_dt, base 16-byte aligned,
+ *            strides multiples of 8 elements.
+ *   lse      [n_new, n_kv_heads*q_per_kv] float, dense, or NULL.
+ *   ws       scratch of squat_paged_attention_workspace(...) bytes for the same
+ *            arguments, 256-byte aligned (NULL where that is 0).
+ * Products of queries and codes or keys are taken in fp16 with sums in fp32
+ * (bf16 queries are brought into fp16's range by a power of two per row first);
+ * statistics of the softmax and the result are held in fp32 until the end.
+ * ------------------------------------------------------------------------- */
+size_t squat_paged_attention_workspace(const squat_paged_store* store, int n_seqs, int64_t n_new, int q_per_kv,
+                                       int pages_per_seq, int64_t max_new, int64_t max_kv);
+
+int squat_paged_attention(const squat_paged_store* store, const void* q, squat_dtype q_dt, int64_t n_new, int q_per_kv,
+                          int64_t q_stride_token, int64_t q_stride_head, const int32_t* q_start, const int32_t* kv_len,
+                          const int32_t* pages, int64_t page_stride, int pages_per_seq, int n_seqs, int64_t max_new,
+                          int64_t max_kv, float out_scale, void* out, int64_t o_stride_token, int64_t o_stride_head,
+                          float* lse, void* ws, size_t ws_bytes, squat_stream stream);
+
+/* ------------------------------------------------------------------------- *
+ * squat_verify_drafts  -- the decision on drafted tokens, from given random
+ * numbers: which of them stand as if the target had drawn them, and the token
+ * that follows.
+ *
+ * For a sequence with drafts x_0 .. x_{n-1} drawn from q_0 .. q_{n-1} and the
+ * target's probabilities p_0 .. p_n at the same positions: draft i is accepted
+ * while  u_i * q_i(x_i) < p_i(x_i).  At the first refusal j the next token comes
+ * from r = max(p_j - q_j, 0) (from p_j itself where r is zero everywhere), after
+ * n acceptances from r = p_n: it is the smallest token whose running sum of r is
+ * over  u_next * (the sum of all of r).  Comparisons and sums are made in 64
+ * bits, so rows need not be normalised.  A row without a positive entry gives 0.
+ *
+ *   tokens   [n_seqs, n_drafts] int64, dense.  A token outside [0, vocab) is refused.
+ *   target   [n_seqs, n_drafts + 1, vocab] dtype dt, vocabulary contiguous, rows
+ *            at s*t_stride_seq + i*t_stride_pos elements.  Entries >= 0.
+ *   draft    [n_seqs, n_drafts, vocab] likewise, or NULL for drafts that were
+ *            chosen outright (q_i is 1 at x_i and 0 elsewhere).
+ *   u        [n_seqs, n_drafts] float, dense, u_next [n_seqs] float, in [0, 1).
+ *   n_draft  [n_seqs] int32, how many of a sequence's drafts count (entries are
+ *            brought into 0 .. n_drafts), or NULL: all.
+ *   accepted out [n_seqs] int32.
+ *   out      out [n_seqs, n_drafts + 1] int64: the accepted drafts, the next
+ *            token, then -1.
+ *   ws       scratch of squat_verify_drafts_workspace(...) bytes, 256-byte aligned.
+ *   0 <= n_drafts <= 64;  1 <= vocab < 2^31 - 4096;  n_seqs <= 65535.
+ * ------------------------------------------------------------------------- */
+size_t squat_verify_drafts_workspace(int n_seqs, int64_t vocab);
+
+int squat_verify_drafts(const int64_t* tokens, int n_seqs, int n_drafts, int64_t vocab, const void* target,
+                        int64_t t_stride_seq, int64_t t_stride_pos, const void* draft, int64_t d_stride_seq,
+                        int64_t d_stride_pos, squat_dtype dt, const float* u, const float* u_next,
+                        const int32_t* n_draft, int32_t* accepted, int64_t* out, void* ws, size_t ws_bytes,
+                        squat_stream stream);
 
 #ifdef __cplusplus
 }

@@ -20,7 +20,7 @@ REFUSING = ("squat_subspace.hip", "_refusing", ("-DSQUAT_TRI_REFUSED(exponent)=(
 
 SOURCES = ["squat_api.cpp", "squat_quantize.hip", "squat_quantize_pc.hip", "squat_dequantize.hip",
            "squat_subspace.hip", "squat_prepare.hip", "squat_scores.hip", "squat_scores_pc.hip", "squat_scores_rope.hip",
-           "squat_cache.hip"]
+           "squat_cache.hip", "squat_paged.hip", "squat_attend.hip", "squat_verify.hip"]
 
 # Packed-fp32 VALU ops are switched off on purpose: some of their forms have given wrong results on this
 # hardware now and then, silently; the kernels' vector budget is therefore 64 lanes per CU and clock.
@@ -42,7 +42,8 @@ def _hipcc() -> str:
 EXTRA = {"squat_prepare.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
          "squat_scores.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
          "squat_scores_pc.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
-         "squat_scores_rope.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+         "squat_scores_rope.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+         "squat_attend.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def _compile(src: str, suffix: str = "", extra=()) -> str:

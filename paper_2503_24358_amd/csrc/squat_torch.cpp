@@ -406,6 +406,257 @@ PyObject* cache_key_scores(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// ---- paged stores and drafted tokens
+
+void need_type(const at::Tensor& t, at::ScalarType type, const char* message) {
+    if (t.scalar_type() != type || !t.is_contiguous()) raise(PyExc_ValueError, message);
+}
+
+// key_codes, key_meta, value_codes, value_meta, bits, group
+squat_paged_store paged_store(PyObject* const* a) {
+    const at::Tensor &kc = tensor(a[0]), &km = tensor(a[1]), &vc = tensor(a[2]), &vm = tensor(a[3]);
+    const at::Tensor* all[4] = {&kc, &km, &vc, &vm};
+    for (const at::Tensor* t : all) need_device(*t);
+    squat_paged_store s;
+    s.bits = small(a[4]);
+    s.group = small(a[5]);
+    need_dims(kc, 4);
+    s.n_pages = kc.size(0);
+    s.n_kv_heads = static_cast<int>(kc.size(1));
+    s.page_tokens = static_cast<int>(kc.size(2));
+    if (kc.size(1) > INT32_MAX || kc.size(2) > INT32_MAX) raise(PyExc_OverflowError, "integer out of range");
+    if (s.group <= 0) raise(PyExc_ValueError, "group must be 32, 64 or 128");
+    const int64_t d = channels(kc.size(3), s.bits);
+    s.d = static_cast<int>(d);
+    const int64_t meta[5] = {kc.size(0), kc.size(1), kc.size(2), d / s.group, 2};
+    if (vc.sizes() != kc.sizes() || km.sizes() != at::IntArrayRef(meta) || vm.sizes() != at::IntArrayRef(meta))
+        raise(PyExc_ValueError, "codes [pages, heads, page, 128*bits/32] and meta [pages, heads, page, 128/group, 2] of keys and values expected");
+    need_type(kc, at::kInt, "codes must be dense int32");
+    need_type(vc, at::kInt, "codes must be dense int32");
+    need_type(km, at::kHalf, "meta must be dense float16");
+    need_type(vm, at::kHalf, "meta must be dense float16");
+    s.key_codes = pointer<uint32_t>(kc);
+    s.key_meta = pointer<uint16_t>(km);
+    s.value_codes = pointer<uint32_t>(vc);
+    s.value_meta = pointer<uint16_t>(vm);
+    return s;
+}
+
+// The stride of a dimension; one of a single entry has none that matters, and gets `dense`.
+int64_t step(const at::Tensor& t, int64_t dim, int64_t dense) { return t.size(dim) > 1 ? t.stride(dim) : dense; }
+
+// Whether two tensors of one shape [tokens, heads, d] are laid out alike.
+bool alike(const at::Tensor& a, const at::Tensor& b) {
+    return step(a, 0, 0) == step(b, 0, 0) && step(a, 1, 0) == step(b, 1, 0) && step(a, 2, 1) == step(b, 2, 1);
+}
+
+// A workspace: the caller's (None: made by the call).
+at::Tensor workspace(PyObject* o) {
+    if (o == Py_None) return {};
+    const at::Tensor& t = tensor(o);
+    need_device(t);
+    if (t.scalar_type() != at::kByte || !t.is_contiguous()) raise(PyExc_ValueError, "ws must be dense uint8");
+    return t;
+}
+
+void make_workspace(at::Tensor& ws, size_t bytes, const at::Tensor& like) {
+    if (!ws.defined() && bytes) ws = empty({static_cast<int64_t>(bytes)}, at::kByte, like);
+}
+
+void* ws_pointer(const at::Tensor& ws) { return ws.defined() ? ws.data_ptr() : nullptr; }
+size_t ws_bytes(const at::Tensor& ws) { return ws.defined() ? static_cast<size_t>(ws.numel()) : 0; }
+
+// k, v, slots, key_codes, key_meta, value_codes, value_meta, bits, group, update, g, ws, stream
+PyObject* paged_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 13, [&]() -> PyObject* {
+        const at::Tensor &k = tensor(a[0]), &v = tensor(a[1]), &slots = tensor(a[2]);
+        need_device(k);
+        need_device(v);
+        need_device(slots);
+        const squat_paged_store st = paged_store(a + 3);
+        need_dims(k, 3);
+        if (k.size(1) != st.n_kv_heads || k.size(2) != st.d || v.sizes() != k.sizes() || v.scalar_type() != k.scalar_type())
+            raise(PyExc_ValueError, "k and v must be [tokens, heads, d] of one dtype");
+        if (!alike(k, v) || (k.numel() && k.stride(2) != 1))
+            raise(PyExc_ValueError, "k and v must share their strides, with unit channel stride");
+        need_type(slots, at::kLong, "slots must be dense int64");
+        if (slots.numel() != k.size(0)) raise(PyExc_ValueError, "one slot per token is needed");
+        const float* update = nullptr;
+        if (a[9] != Py_None) {
+            const at::Tensor& u = tensor(a[9]);
+            need_device(u);
+            need_type(u, at::kFloat, "update must be dense float32");
+            if (u.sizes() != at::IntArrayRef({st.n_kv_heads, st.d, st.d})) raise(PyExc_ValueError, "update must be [heads, d, d]");
+            update = pointer<const float>(u);
+        }
+        const int g = small(a[10]);
+        at::Tensor ws = workspace(a[11]);
+        const squat_dtype dt = dtype(a[0], k);
+        const squat_stream s = stream(a[12]);
+        call("squat_paged_write", [&] {
+            if (update) make_workspace(ws, squat_paged_write_workspace(&st, k.size(0), 1), k);
+            return squat_paged_write(&st, k.data_ptr(), v.data_ptr(), dt, k.size(0), step(k, 0, k.size(1) * st.d), step(k, 1, st.d),
+                                     pointer<const int64_t>(slots), update, g, ws_pointer(ws), ws_bytes(ws), s);
+        });
+        Py_RETURN_NONE;
+    });
+}
+
+// slots, key_codes, key_meta, value_codes, value_meta, bits, group, out_dtype, k, v, stream
+PyObject* paged_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 11, [&]() -> PyObject* {
+        const at::Tensor& slots = tensor(a[0]);
+        need_device(slots);
+        need_type(slots, at::kLong, "slots must be dense int64");
+        const squat_paged_store st = paged_store(a + 1);
+        if (!THPDtype_Check(a[7])) raise(PyExc_TypeError, "out_dtype must be a torch.dtype");
+        const at::ScalarType type = reinterpret_cast<THPDtype*>(a[7])->scalar_type;
+        at::Tensor k = given(a[8], slots), v = given(a[9], slots);
+        const int64_t tokens = slots.numel();
+        for (const at::Tensor* t : {&k, &v})
+            if (t->defined() && (t->dim() != 3 || t->size(0) != tokens || t->size(1) != st.n_kv_heads || t->size(2) != st.d ||
+                                 t->scalar_type() != type || (t->numel() && t->stride(2) != 1)))
+                raise(PyExc_ValueError, "k and v must be [tokens, heads, d] of out_dtype with unit channel stride");
+        if (k.defined() && v.defined() && !alike(k, v)) raise(PyExc_ValueError, "k and v must share their strides");
+        squat_dtype dt;
+        switch (type) {
+            case at::kFloat: dt = SQUAT_F32; break;
+            case at::kHalf: dt = SQUAT_F16; break;
+            case at::kBFloat16: dt = SQUAT_BF16; break;
+            default: raise(PyExc_ValueError, "out_dtype must be float32, float16 or bfloat16");
+        }
+        const squat_stream s = stream(a[10]);
+        call("squat_paged_read", [&] {
+            const at::Tensor& other = k.defined() ? k : v;
+            const auto make = [&] {
+                at::Tensor t = empty({tokens, st.n_kv_heads, st.d}, type, slots);
+                return other.defined() && !alike(t, other) ? at::Tensor() : t;
+            };
+            if (!k.defined()) k = make();
+            if (!v.defined()) v = make();
+            if (!k.defined() || !v.defined()) return static_cast<int>(SQUAT_E_BADSHAPE);        // one given, strided: the other must be too
+            return squat_paged_read(&st, pointer<const int64_t>(slots), tokens, k.data_ptr(), v.data_ptr(), dt, step(k, 0, k.size(1) * st.d),
+                                    step(k, 1, st.d), s);
+        });
+        PyObject *pk = THPVariable_Wrap(k), *pv = pk ? THPVariable_Wrap(v) : nullptr;
+        PyObject* out = pv ? PyTuple_Pack(2, pk, pv) : nullptr;
+        Py_XDECREF(pk);
+        Py_XDECREF(pv);
+        return out;
+    });
+}
+
+// q, key_codes, key_meta, value_codes, value_meta, bits, group, pages, kv_len, q_start, out_scale, max_new, max_kv, out, lse, ws, stream
+PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 17, [&]() -> PyObject* {
+        const at::Tensor &q = tensor(a[0]), &pages = tensor(a[7]), &kv_len = tensor(a[8]), &q_start = tensor(a[9]);
+        need_device(q);
+        need_device(pages);
+        need_device(kv_len);
+        need_device(q_start);
+        const squat_paged_store st = paged_store(a + 1);
+        need_dims(q, 3);
+        if (st.n_kv_heads < 1 || q.size(1) < 1 || q.size(1) % st.n_kv_heads || q.size(2) != st.d || (q.numel() && q.stride(2) != 1))
+            raise(PyExc_ValueError, "q must be [tokens, heads * q_per_kv, d] with unit channel stride");
+        const int64_t seqs = kv_len.numel();
+        if (pages.dim() != 2 || pages.scalar_type() != at::kInt || pages.size(0) != seqs || (pages.size(1) > 1 && pages.stride(1) != 1))
+            raise(PyExc_ValueError, "pages must be int32 [sequences, pages] with unit stride");
+        need_type(kv_len, at::kInt, "kv_len must be dense int32");
+        need_type(q_start, at::kInt, "q_start must be dense int32");
+        if (q_start.numel() != seqs + 1) raise(PyExc_ValueError, "q_start must have one entry more than kv_len");
+        if (seqs > INT32_MAX || pages.size(1) > INT32_MAX) raise(PyExc_OverflowError, "integer out of range");
+        at::Tensor out = given(a[13], q);
+        if (out.defined() && (out.sizes() != q.sizes() || out.scalar_type() != q.scalar_type() || (out.numel() && out.stride(2) != 1)))
+            raise(PyExc_ValueError, "out must have q's shape and dtype and unit channel stride");
+        float* lse = nullptr;
+        if (a[14] != Py_None) {
+            const at::Tensor& l = tensor(a[14]);
+            need_device(l);
+            need_type(l, at::kFloat, "lse must be dense float32");
+            if (l.dim() != 2 || l.size(0) != q.size(0) || l.size(1) != q.size(1)) raise(PyExc_ValueError, "lse must be [tokens, query heads]");
+            lse = pointer<float>(l);
+        }
+        at::Tensor ws = workspace(a[15]);
+        const float scale = number(a[10]);
+        const int64_t max_new = integer(a[11]), max_kv = integer(a[12]);
+        const squat_dtype dt = dtype(a[0], q);
+        const squat_stream s = stream(a[16]);
+        const int64_t tokens = q.size(0);
+        const int qpk = static_cast<int>(q.size(1) / st.n_kv_heads), width = static_cast<int>(pages.size(1));
+        call("squat_paged_attention", [&] {
+            if (!out.defined()) out = empty(q.sizes(), q.scalar_type(), q);
+            make_workspace(ws, squat_paged_attention_workspace(&st, static_cast<int>(seqs), tokens, qpk, width, max_new, max_kv), q);
+            const int64_t row = q.size(1) * st.d;
+            return squat_paged_attention(&st, q.data_ptr(), dt, tokens, qpk, step(q, 0, row), step(q, 1, st.d), pointer<const int32_t>(q_start),
+                                         pointer<const int32_t>(kv_len), pointer<const int32_t>(pages), step(pages, 0, width), width,
+                                         static_cast<int>(seqs), max_new, max_kv, scale, out.data_ptr(), step(out, 0, row), step(out, 1, st.d), lse,
+                                         ws_pointer(ws), ws_bytes(ws), s);
+        });
+        return a[13] == Py_None ? THPVariable_Wrap(out) : Py_NewRef(a[13]);
+    });
+}
+
+// tokens, target, draft, u, u_next, n_draft, accepted, out, ws, stream
+PyObject* verify_drafts(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 10, [&]() -> PyObject* {
+        const at::Tensor &tokens = tensor(a[0]), &target = tensor(a[1]), &u = tensor(a[3]), &u_next = tensor(a[4]);
+        for (const at::Tensor* t : {&tokens, &target, &u, &u_next}) need_device(*t);
+        need_dims(tokens, 2);
+        need_dims(target, 3);
+        const int64_t seqs = tokens.size(0), drafts = tokens.size(1), vocab = target.size(2);
+        if (seqs > INT32_MAX || drafts > INT32_MAX) raise(PyExc_OverflowError, "integer out of range");
+        need_type(tokens, at::kLong, "tokens must be dense int64");
+        if (target.size(0) != seqs || target.size(1) != drafts + 1 || (vocab > 1 && target.stride(2) != 1))
+            raise(PyExc_ValueError, "target must be [sequences, drafts + 1, vocabulary] with unit stride");
+        need_type(u, at::kFloat, "u must be dense float32");
+        need_type(u_next, at::kFloat, "u_next must be dense float32");
+        if (u.sizes() != tokens.sizes() || u_next.numel() != seqs) raise(PyExc_ValueError, "u must be [sequences, drafts], u_next [sequences]");
+        const void* dp = nullptr;
+        int64_t ds = 0, dpos = 0;
+        if (a[2] != Py_None) {
+            const at::Tensor& d = tensor(a[2]);
+            need_device(d);
+            if (d.sizes() != at::IntArrayRef({seqs, drafts, vocab}) || d.scalar_type() != target.scalar_type() || (vocab > 1 && d.numel() && d.stride(2) != 1))
+                raise(PyExc_ValueError, "draft must be [sequences, drafts, vocabulary] of target's dtype with unit stride");
+            dp = drafts ? d.data_ptr() : nullptr;
+            ds = d.stride(0);
+            dpos = d.stride(1);
+        }
+        const int32_t* np = nullptr;
+        if (a[5] != Py_None) {
+            const at::Tensor& t = tensor(a[5]);
+            need_device(t);
+            need_type(t, at::kInt, "n_draft must be dense int32");
+            if (t.numel() != seqs) raise(PyExc_ValueError, "n_draft must be [sequences]");
+            np = pointer<const int32_t>(t);
+        }
+        at::Tensor accepted = given(a[6], tokens), out = given(a[7], tokens), ws = workspace(a[8]);
+        if (accepted.defined()) {
+            need_type(accepted, at::kInt, "accepted must be dense int32");
+            if (accepted.numel() != seqs) raise(PyExc_ValueError, "accepted must be [sequences]");
+        }
+        if (out.defined()) {
+            need_type(out, at::kLong, "out must be dense int64");
+            if (out.dim() != 2 || out.size(0) != seqs || out.size(1) != drafts + 1) raise(PyExc_ValueError, "out must be [sequences, drafts + 1]");
+        }
+        const squat_dtype dt = dtype(a[1], target);
+        const squat_stream s = stream(a[9]);
+        call("squat_verify_drafts", [&] {
+            if (!accepted.defined()) accepted = empty({seqs}, at::kInt, tokens);
+            if (!out.defined()) out = empty({seqs, drafts + 1}, at::kLong, tokens);
+            make_workspace(ws, squat_verify_drafts_workspace(static_cast<int>(seqs), vocab), tokens);
+            return squat_verify_drafts(pointer<const int64_t>(tokens), static_cast<int>(seqs), static_cast<int>(drafts), vocab, target.data_ptr(),
+                                       target.stride(0), target.stride(1), dp, ds, dpos, dt, pointer<const float>(u), pointer<const float>(u_next),
+                                       np, pointer<int32_t>(accepted), pointer<int64_t>(out), ws_pointer(ws), ws_bytes(ws), s);
+        });
+        PyObject *pa = THPVariable_Wrap(accepted), *po = pa ? THPVariable_Wrap(out) : nullptr;
+        PyObject* both = po ? PyTuple_Pack(2, pa, po) : nullptr;
+        Py_XDECREF(pa);
+        Py_XDECREF(po);
+        return both;
+    });
+}
+
 PyObject* set_error(PyObject*, PyObject* cls) {
     Py_XINCREF(cls);
     Py_XSETREF(squat_error, cls);
@@ -425,6 +676,10 @@ PyMethodDef methods[] = {
     SQUAT_FAST("cache_append", cache_append),
     SQUAT_FAST("cache_key_scores", cache_key_scores<false>),
     SQUAT_FAST("cache_key_scores_rope", cache_key_scores<true>),
+    SQUAT_FAST("paged_write", paged_write),
+    SQUAT_FAST("paged_read", paged_read),
+    SQUAT_FAST("paged_attention", paged_attention),
+    SQUAT_FAST("verify_drafts", verify_drafts),
     {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 

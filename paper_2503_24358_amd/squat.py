@@ -28,7 +28,9 @@ SYMBOLS = ("squat_version", "squat_strerror", "squat_build_subspace_workspace",
            "squat_key_scores_rope_per_channel",
            "squat_cache_arena_bytes", "squat_cache_create", "squat_cache_destroy", "squat_cache_reset",
            "squat_cache_state", "squat_cache_get_buffers", "squat_cache_prefill", "squat_cache_append",
-           "squat_cache_key_scores", "squat_cache_key_scores_rope")
+           "squat_cache_key_scores", "squat_cache_key_scores_rope",
+           "squat_paged_write_workspace", "squat_paged_write", "squat_paged_read", "squat_paged_attention_workspace",
+           "squat_paged_attention", "squat_verify_drafts_workspace", "squat_verify_drafts")
 
 
 class CacheConfig(ctypes.Structure):
@@ -54,6 +56,13 @@ class CacheCounts(ctypes.Structure):
 class QuantizePlan(ctypes.Structure):
     _fields_ = [("problems", ctypes.c_int64), ("workgroups_per_problem", ctypes.c_int),
                 ("wavefronts_per_workgroup", ctypes.c_int), ("tiles_per_problem", ctypes.c_int64)]
+
+
+class PagedStoreArrays(ctypes.Structure):
+    """squat_paged_store: device pointers and sizes."""
+    _fields_ = [("key_codes", ctypes.c_void_p), ("key_meta", ctypes.c_void_p), ("value_codes", ctypes.c_void_p),
+                ("value_meta", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("n_kv_heads", ctypes.c_int),
+                ("page_tokens", ctypes.c_int), ("d", ctypes.c_int), ("bits", ctypes.c_int), ("group", ctypes.c_int)]
 
 
 class SquatError(RuntimeError):
@@ -137,6 +146,22 @@ def lib() -> ctypes.CDLL:
     L.squat_cache_key_scores.argtypes = [vp, vp, i32, i64, i64, f32, vp, i64, i64, vp]
     L.squat_cache_key_scores_rope.restype = i32
     L.squat_cache_key_scores_rope.argtypes = [vp, vp, i32, i64, i64, vp, i64, f32, vp, i64, i64, vp]
+    storep = ctypes.POINTER(PagedStoreArrays)
+    L.squat_paged_write_workspace.restype = sz
+    L.squat_paged_write_workspace.argtypes = [storep, i64, i32]
+    L.squat_paged_write.restype = i32
+    L.squat_paged_write.argtypes = [storep, vp, vp, i32, i64, i64, i64, vp, vp, i32, vp, sz, vp]
+    L.squat_paged_read.restype = i32
+    L.squat_paged_read.argtypes = [storep, vp, i64, vp, vp, i32, i64, i64, vp]
+    L.squat_paged_attention_workspace.restype = sz
+    L.squat_paged_attention_workspace.argtypes = [storep, i32, i64, i32, i32, i64, i64]
+    L.squat_paged_attention.restype = i32
+    L.squat_paged_attention.argtypes = [storep, vp, i32, i64, i32, i64, i64, vp, vp, vp, i64, i32, i32, i64, i64, f32, vp, i64, i64,
+                                        vp, vp, sz, vp]
+    L.squat_verify_drafts_workspace.restype = sz
+    L.squat_verify_drafts_workspace.argtypes = [i32, i64]
+    L.squat_verify_drafts.restype = i32
+    L.squat_verify_drafts.argtypes = [vp, i32, i32, i64, vp, i64, i64, vp, i64, i64, i32, vp, vp, vp, vp, vp, vp, sz, vp]
     _lib = L
     return L
 
@@ -496,3 +521,66 @@ class Cache:
         inv_freq: [d/2] float32 on the device."""
         return (_native or native()).cache_key_scores_rope(self._h and self._h.value, q, inv_freq, int(pos0), out_scale, out,
                                                            None if stream is None else _stream(stream))
+
+
+def paged_write(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, key_codes: torch.Tensor, key_meta: torch.Tensor,
+                value_codes: torch.Tensor, value_meta: torch.Tensor, bits: int, group: int, *, update=None, g: int = 32, ws=None,
+                stream=None) -> None:
+    """squat_paged_write: quantizes the keys and values [tokens, heads, d] of new tokens into their slots (int64 [tokens]: page *
+    page_tokens + offset; one outside the store: the token is skipped).  Store: codes int32 [pages, heads, page, d*bits/32], meta
+    float16 [pages, heads, page, d/group, 2].  update: float32 [heads, d, d] as written by prepare for this g (bits 2 or 4), or None."""
+    (_native or native()).paged_write(k, v, slots, key_codes, key_meta, value_codes, value_meta, bits, group, update, g, ws,
+                                      None if stream is None else _stream(stream))
+
+
+def paged_read(slots: torch.Tensor, key_codes: torch.Tensor, key_meta: torch.Tensor, value_codes: torch.Tensor,
+               value_meta: torch.Tensor, bits: int, group: int, out_dtype=torch.bfloat16, *, k=None, v=None, stream=None):
+    """squat_paged_read: (keys, values) [tokens, heads, d] that the store holds in `slots`; zeros for a slot outside the store."""
+    return (_native or native()).paged_read(slots, key_codes, key_meta, value_codes, value_meta, bits, group, out_dtype, k, v,
+                                            None if stream is None else _stream(stream))
+
+
+def paged_attention(q: torch.Tensor, key_codes: torch.Tensor, key_meta: torch.Tensor, value_codes: torch.Tensor,
+                    value_meta: torch.Tensor, bits: int, group: int, pages: torch.Tensor, kv_len: torch.Tensor, q_start: torch.Tensor,
+                    out_scale: float, *, max_new: int = 0, max_kv: int = 0, out=None, lse=None, ws=None, stream=None) -> torch.Tensor:
+    """squat_paged_attention: q [new tokens, heads*q_per_kv, d] (fp16 or bf16) of all sequences behind each other, sequence s's being
+    q_start[s] .. q_start[s+1] (int32 [sequences + 1]), the last of its kv_len[s] tokens (int32) in pages[s] (int32 [sequences,
+    pages]); a new token sees itself and everything before it.  max_new, max_kv: the largest number of new tokens and the largest kv_len,
+    where known (0: not).  lse: float32 [new tokens, query heads], filled if given.  Returns q's shape and dtype."""
+    return (_native or native()).paged_attention(q, key_codes, key_meta, value_codes, value_meta, bits, group, pages, kv_len, q_start,
+                                                 out_scale, max_new, max_kv, out, lse, ws, None if stream is None else _stream(stream))
+
+
+def verify_drafts(tokens: torch.Tensor, target: torch.Tensor, draft: Optional[torch.Tensor], u: torch.Tensor, u_next: torch.Tensor, *,
+                  n_draft=None, accepted=None, out=None, ws=None, stream=None):
+    """squat_verify_drafts: drafted tokens (int64 [sequences, drafts]) against the target's probabilities [sequences, drafts + 1,
+    vocabulary] and the drafts' own [sequences, drafts, vocabulary] (None: the drafts were chosen outright), decided by the random
+    numbers u [sequences, drafts] and u_next [sequences] (float32 in [0, 1)).  n_draft: int32 [sequences], how many drafts count.
+    Returns (accepted int32 [sequences], tokens int64 [sequences, drafts + 1]: the accepted drafts, the next token, then -1)."""
+    return (_native or native()).verify_drafts(tokens, target, draft, u, u_next, n_draft, accepted, out, ws,
+                                               None if stream is None else _stream(stream))
+
+
+class PagedStore:
+    """The arrays of a paged store and the calls on it.  Which page belongs to which sequence is the caller's to say."""
+
+    def __init__(self, n_pages: int, n_kv_heads: int, page_tokens: int, bits: int, group: int, device="cuda", d: int = 128):
+        self.bits, self.group, self.page_tokens = bits, group, page_tokens
+        codes, meta = (n_pages, n_kv_heads, page_tokens, d * bits // 32), (n_pages, n_kv_heads, page_tokens, d // group, 2)
+        self.key_codes = torch.zeros(codes, dtype=torch.int32, device=device)
+        self.key_meta = torch.zeros(meta, dtype=torch.float16, device=device)
+        self.value_codes = torch.zeros(codes, dtype=torch.int32, device=device)
+        self.value_meta = torch.zeros(meta, dtype=torch.float16, device=device)
+
+    @property
+    def arrays(self):
+        return self.key_codes, self.key_meta, self.value_codes, self.value_meta, self.bits, self.group
+
+    def write(self, k, v, slots, **kw):
+        paged_write(k, v, slots, *self.arrays, **kw)
+
+    def read(self, slots, out_dtype=torch.bfloat16, **kw):
+        return paged_read(slots, *self.arrays, out_dtype, **kw)
+
+    def attention(self, q, pages, kv_len, q_start, out_scale, **kw):
+        return paged_attention(q, *self.arrays, pages, kv_len, q_start, out_scale, **kw)

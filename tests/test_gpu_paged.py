@@ -1,0 +1,228 @@
+"""squat_paged_write and squat_paged_read against their definition in 64 bits (paged_ref): codes, scales and zero-points equal, what is
+read back within one rounding of code * scale + zero."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2503_24358_amd import squat, synth
+from tests import paged_ref as P
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+
+
+def _store(n_pages, heads, page, bits, group, fill=0):
+    s = squat.PagedStore(n_pages, heads, page, bits, group)
+    for t in (s.key_codes, s.value_codes):
+        t.fill_(fill)
+    return s
+
+
+def _host(t):
+    return t.cpu().numpy()
+
+
+def _rows(store, slots, page):
+    """(key codes, key meta, value codes, value meta) at the slots, numpy [n, heads, ...]."""
+    at, off = slots // page, slots % page
+    return [_host(t)[at, :, off] for t in (store.key_codes, store.key_meta, store.value_codes, store.value_meta)]
+
+
+def _check(k, v, store, slots, page, bits, group):
+    kc, km, vc, vm = _rows(store, slots, page)
+    for x, c, m in ((k, kc, km), (v, vc, vm)):
+        want_c, want_m = P.quantize(x.double().cpu().numpy(), bits, group)
+        assert np.array_equal(m.view(np.uint16), want_m.view(np.uint16))
+        assert np.array_equal(P.unpack(c, bits), want_c)
+
+
+def _read_ok(got, codes, meta, bits):
+    want = P.values(codes, meta, bits)
+    g = got.double().cpu().numpy()
+    tol = torch.finfo(got.dtype).eps / 2 * np.abs(want) * 1.001 + np.abs(want).max() * 2.0 ** -24 + torch.finfo(got.dtype).smallest_normal
+    assert (np.abs(g - want) <= tol).all()
+
+
+@pytest.mark.parametrize("bits", [2, 4, 8])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_write_and_read(bits, group, dtype):
+    g = torch.Generator().manual_seed(bits * 1000 + group)
+    for n, heads, page in ((1, 1, 16), (33, 3, 32), (257, 2, 64)):
+        k = (torch.randn(n, heads, 128, generator=g) * 3).to(DT[dtype]).cuda()
+        v = torch.randn(n, heads, 128, generator=g).to(DT[dtype]).cuda()
+        pages = -(-n // page) + 2
+        slots = torch.randperm(pages * page, generator=g)[:n]
+        s = _store(pages, heads, page, bits, group)
+        s.write(k, v, slots.cuda())
+        _check(k, v, s, slots.numpy(), page, bits, group)
+        for out in (torch.bfloat16, torch.float16, torch.float32):
+            rk, rv = s.read(slots.cuda(), out)
+            kc, km, vc, vm = _rows(s, slots.numpy(), page)
+            _read_ok(rk, kc, km, bits)
+            _read_ok(rv, vc, vm, bits)
+
+
+@pytest.mark.parametrize("bits", [2, 4, 8])
+def test_write_at_rounding_borders(bits):
+    """Values that lie on (k + 1/2) steps exactly and one step of the input's type beside them; constant groups; tiny and large ranges."""
+    top = (1 << bits) - 1
+    rows = []
+    for step in (1.0, 0.5, 2.0 ** -10, 3.0, 2.0 ** -24, 96.0):
+        base = np.array([0.0, top * step] + [(i % top + 0.5) * step for i in range(126)])
+        rows += [base, np.nextafter(base.astype(np.float16), np.float16(np.inf)).astype(np.float64),
+                 np.nextafter(base.astype(np.float16), np.float16(-np.inf)).astype(np.float64), base - 5 * step]
+    rows += [np.zeros(128), np.full(128, 1.5), np.full(128, -60000.0), np.linspace(-65000, 65000, 128), np.linspace(-1e-6, 1e-6, 128),
+             np.r_[np.full(127, 1000.0), 1000.5], np.r_[np.full(127, 6e-8), 0.0]]
+    x = torch.from_numpy(np.array(rows)).float()
+    for dtype in (torch.float16, torch.float32):
+        k = x.to(dtype).view(-1, 1, 128).cuda()
+        for group in (32, 128):
+            s = _store(4, 1, 16, bits, group)
+            slots = torch.arange(len(rows))
+            s.write(k, k.flip(2).contiguous(), slots.cuda())
+            _check(k, k.flip(2), s, slots.numpy(), 16, bits, group)
+
+
+def test_slots_outside_the_store_are_skipped_and_read_as_zeros():
+    k = torch.randn(6, 2, 128).bfloat16().cuda()
+    s = _store(2, 2, 16, 4, 32, fill=0x5A5A5A5A)
+    slots = torch.tensor([-1, 3, 32, 31, 1 << 40, -(1 << 40)]).cuda()
+    s.write(k, k, slots)
+    used = np.zeros((2, 16), bool)
+    used[0, 3] = used[1, 15] = True
+    codes = _host(s.key_codes).transpose(0, 2, 1, 3)
+    assert (codes[~used] == 0x5A5A5A5A).all() and (_host(s.key_meta).transpose(0, 2, 1, 3, 4)[~used] == 0).all()
+    _check(k[[1, 3]], k[[1, 3]], s, np.array([3, 31]), 16, 4, 32)
+    rk, rv = s.read(slots, torch.float32)
+    for r in (rk, rv):
+        assert (r[[0, 2, 4, 5]] == 0).all() and (r[[1, 3]] != 0).any()
+
+
+@pytest.mark.parametrize("bits", [2, 4, 8])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_a_value_that_is_not_finite_spoils_its_own_group_alone(bits, dtype):
+    k = torch.randn(4, 2, 128).to(DT[dtype])
+    k[1, 0, 40] = float("nan")
+    k[2, 1, 0] = float("inf")
+    k[3, 1, 127] = float("-inf")
+    v = torch.randn(4, 2, 128).to(DT[dtype])
+    s = _store(1, 2, 16, bits, 32)
+    s.write(k.cuda(), v.cuda(), torch.arange(4).cuda())
+    rk, rv = s.read(torch.arange(4).cuda(), torch.float32)
+    bad = torch.zeros(4, 2, 4, dtype=torch.bool)
+    bad[1, 0, 1] = bad[2, 1, 0] = bad[3, 1, 3] = True
+    assert torch.equal(rk.cpu().view(4, 2, 4, 32).isfinite(), ~bad.unsqueeze(-1).expand(-1, -1, -1, 32))
+    assert rv.isfinite().all()
+    clean = k.clone()
+    clean.view(4, 2, 4, 32)[bad] = 0
+    t = _store(1, 2, 16, bits, 32)
+    t.write(clean.cuda(), v.cuda(), torch.arange(4).cuda())
+    ck, _ = t.read(torch.arange(4).cuda(), torch.float32)
+    assert torch.equal(rk.view(4, 2, 4, 32)[~bad.cuda()], ck.view(4, 2, 4, 32)[~bad.cuda()])
+
+
+def test_strides():
+    """Keys and values as slices of one projection's output; outputs inside a larger tensor."""
+    qkv = torch.randn(37, 3, 5, 128).half().cuda()                # [tokens, (q, k, v), heads, d]
+    k, v = qkv[:, 1], qkv[:, 2]
+    heads_first = torch.randn(2, 5, 37, 128).half().cuda().transpose(1, 2)
+    slots = torch.arange(5, 42).cuda()
+    for a, b in ((k, v), (heads_first[0], heads_first[1])):
+        s = _store(3, 5, 16, 4, 64)
+        s.write(a, b, slots)
+        _check(a, b, s, slots.cpu().numpy(), 16, 4, 64)
+        big = torch.full((2, 37, 7, 5, 136), 7.0, device="cuda")
+        s.read(slots, torch.float32, k=big[0, :, 3, :, :128], v=big[1, :, 3, :, :128])
+        rk, rv = s.read(slots, torch.float32)
+        assert torch.equal(big[0, :, 3, :, :128], rk) and torch.equal(big[1, :, 3, :, :128], rv)
+        assert (big[..., 128:] == 7).all() and (big[:, :, :3] == 7).all() and (big[:, :, 4:] == 7).all()
+    one = torch.randn(1, 1, 128).half().cuda()
+    s = _store(1, 1, 16, 4, 32)
+    odd = one.as_strided((1, 1, 128), (3, 5, 1))                  # strides of dimensions of one entry do not matter
+    s.write(odd, one, torch.tensor([2]).cuda())
+    _check(one, one, s, np.array([2]), 16, 4, 32)
+
+
+def test_nothing_to_do():
+    s = _store(1, 2, 16, 4, 32)
+    none = torch.empty(0, 2, 128, dtype=torch.half, device="cuda")
+    s.write(none, none, torch.empty(0, dtype=torch.int64, device="cuda"))
+    k, v = s.read(torch.empty(0, dtype=torch.int64, device="cuda"))
+    assert k.shape == (0, 2, 128) and v.shape == (0, 2, 128) and (s.key_codes == 0).all()
+
+
+@pytest.mark.parametrize("bits,group,g", [(2, 32, 32), (4, 64, 64), (4, 128, 32)])
+def test_keys_with_an_update_matrix_are_those_of_quantize_keys(bits, group, g):
+    gen = synth.rng(77)
+    n, heads, page = 75, 3, 32
+    qhat = torch.from_numpy((gen.standard_normal((heads, 16, 128)) * 20).astype(np.float32)).cuda()
+    update = squat.prepare(qhat, 1e-3, g)
+    k, v = torch.randn(n, heads, 128).bfloat16().cuda(), torch.randn(n, heads, 128).bfloat16().cuda()
+    slots = torch.randperm(5 * page)[:n].cuda()
+    s = _store(5, heads, page, bits, group)
+    s.write(k, v, slots, update=update, g=g)
+    codes, scale, zero = squat.quantize_keys(k.transpose(0, 1).unsqueeze(0), update, bits, group, g)
+    kc, km, vc, vm = _rows(s, slots.cpu().numpy(), page)
+    assert np.array_equal(kc, _host(codes)[0].transpose(1, 0, 2))
+    assert np.array_equal(km[..., 0], _host(scale)[0].transpose(1, 0, 2)) and np.array_equal(km[..., 1], _host(zero)[0].transpose(1, 0, 2))
+    want_c, want_m = P.quantize(v.double().cpu().numpy(), bits, group)
+    assert np.array_equal(P.unpack(vc, bits), want_c) and np.array_equal(vm, want_m)
+
+
+def test_another_stream_and_a_graph():
+    k, v = torch.randn(40, 2, 128).half().cuda(), torch.randn(40, 2, 128).half().cuda()
+    slots = torch.randperm(64)[:40].cuda()
+    s = _store(4, 2, 16, 4, 32)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    s.write(k, v, slots, stream=side)
+    rk = torch.empty(40, 2, 128, dtype=torch.float16, device="cuda")
+    rv = torch.empty_like(rk)
+    s.read(slots, torch.float16, k=rk, v=rv, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    _check(k, v, s, slots.cpu().numpy(), 16, 4, 32)
+    with torch.cuda.stream(side):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            s.write(k, v, slots)
+            s.read(slots, torch.float16, k=rk, v=rv)
+    torch.cuda.synchronize()
+    for i in range(4):
+        k.copy_(torch.randn(40, 2, 128))
+        v.copy_(torch.randn(40, 2, 128))
+        graph.replay()
+        torch.cuda.synchronize()
+        _check(k, v, s, slots.cpu().numpy(), 16, 4, 32)
+        ek, ev = s.read(slots, torch.float16)                     # eager work between the replays
+        assert torch.equal(ek, rk) and torch.equal(ev, rv)
+
+
+def test_slots_past_four_gigabytes():
+    """A store whose codes are larger than 2^32 bytes: first and last pages."""
+    heads, page, bits = 8, 256, 8
+    n_pages = (1 << 32) // (heads * page * 128) + 40
+    s = squat.PagedStore.__new__(squat.PagedStore)
+    s.bits, s.group, s.page_tokens = bits, 128, page
+    s.key_codes = torch.empty((n_pages, heads, page, 32), dtype=torch.int32, device="cuda")
+    s.value_codes = torch.empty_like(s.key_codes)
+    s.key_meta = torch.empty((n_pages, heads, page, 1, 2), dtype=torch.float16, device="cuda")
+    s.value_meta = torch.empty_like(s.key_meta)
+    k, v = torch.randn(600, heads, 128).bfloat16().cuda(), torch.randn(600, heads, 128).bfloat16().cuda()
+    slots = torch.cat([torch.arange(300), torch.arange(n_pages * page - 300, n_pages * page)]).cuda()
+    s.write(k, v, slots)
+    rk, rv = s.read(slots, torch.float32)
+    for x, r in ((k, rk), (v, rv)):
+        c, m = P.quantize(x.double().cpu().numpy(), bits, 128)
+        want = P.values(P.pack(c, bits), m, bits)
+        assert np.abs(r.double().cpu().numpy() - want).max() <= np.abs(want).max() * 2.0 ** -23
+    q = torch.randn(2, heads * 2, 128).bfloat16().cuda()
+    pages = torch.tensor([[0, 1], [n_pages - 2, n_pages - 1]], dtype=torch.int32).cuda()
+    out = s.attention(q, pages, torch.tensor([300, 512], dtype=torch.int32).cuda(), torch.tensor([0, 1, 2], dtype=torch.int32).cuda(), 0.1)
+    small = squat.PagedStore(4, heads, page, bits, 128)
+    for a, b in zip(small.arrays[:4], s.arrays[:4]):
+        a.copy_(b[[0, 1, n_pages - 2, n_pages - 1]])
+    same = small.attention(q, torch.tensor([[0, 1], [2, 3]], dtype=torch.int32).cuda(), torch.tensor([300, 512], dtype=torch.int32).cuda(),
+                           torch.tensor([0, 1, 2], dtype=torch.int32).cuda(), 0.1)
+    assert torch.equal(out, same)
