@@ -6,12 +6,10 @@
 // softmax's maximum and sum stay in the lane, and the logits of a lane (tokens 4 h + i of the step's halves, h = lane / 16) are
 // where the second product wants its operand: nothing is exchanged between lanes and nothing goes through LDS.
 //
-// Keys enter as raw integer codes (exact in fp16); scale and zero-point of a group come in behind, in fp32:
-//     q . k_t = sum_g scale[t,g] (sum_{c in g} q_c code_c) + zero[t,g] (sum_{c in g} q_c).
-// Codes are turned into fp16 by placing their bits in the mantissa of a power of two, bias + code, one or two operations per pair;
-// the accumulator starts at -bias sum q.  Values are contracted over tokens, whose scales differ, so they are dequantized, one
-// rounding (2^-11) each; a lane takes 8 channels of 8 tokens, which it needs as 8 operands of 8 tokens, one per channel, so
-// that the order of channels and tokens in the products makes a transpose unnecessary.
+// Codes become fp16 by placing their bits in the mantissa of a power of two (bias + code, one or two operations per pair); less the bias,
+// they are dequantized by one fused multiply-add, one rounding (2^-11), in the lane that holds them: a quarter of a key's channels with
+// one scale, or 8 channels of 8 tokens of the values, which the second product needs as 8 operands of 8 tokens, one per channel.
+// The order of channels and tokens within the products is free, so that neither needs a transpose.
 //
 // The running maximum m of a row is raised only when a logit passes it by more than 2^kSlack (the rows' sums are rescaled then, for
 // all of them): p = 2^(x - m + kLift), at most 2^15, and small weights keep their bits down to 2^-(24 + kLift) of the largest.
@@ -27,6 +25,7 @@ constexpr int kStep = 32;                                 // tokens per step of 
 constexpr int kWaves = 4;
 constexpr float kLift = 11.0f, kSlack = 4.0f;
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
+constexpr int kTarget = 8, kLeast = 8;                    // a launch's workgroups per compute unit, where there is work for them; a part's steps
 constexpr int kPitch = kD + 4;                            // floats per row of a wavefront's sums in LDS
 
 struct AttendParams {
@@ -40,10 +39,31 @@ struct AttendParams {
     int64_t page_stride;
     int pages_per_seq, n_seqs, n_new, n_kv, qpk, n_pages, page_shift;
     float scale;                                          // out_scale * log2(e)
-    int splits, least;                                    // parts of a sequence at most; steps per part at least
+    int splits, span;                                     // parts of a sequence at most, and a part's steps where those are enough
     int n_tiles;
     float* part_o;                                        // [splits, n_tiles, n_kv, rows, d]
     float2* part_ml;                                      // [splits, n_tiles, n_kv, rows]
+};
+
+// A workgroup's place: the KV heads go round fastest (8 of them: a head's pages stay in one XCD's L2), then the sequences' first tiles, then the
+// parts; the further tiles come behind all of these.  The workgroups of an XCD go to its four shader engines in turn, so what may have no work
+// (a tile that is not needed, a short sequence's later parts) must not come at every second or fourth place: one sequence of
+// 131072 tokens 66 -> 37 us, 64 ragged ones 136 -> 83 (104 with the parts before the sequences).
+struct Work {
+    int tile, part, kvh;
+    __device__ __forceinline__ explicit Work(const AttendParams& p) {
+        const uint32_t n = p.n_kv;
+        uint32_t i = blockIdx.x / n;
+        kvh = static_cast<int>(blockIdx.x - i * n);
+        uint32_t tiles = p.n_seqs, from = 0;
+        if (i >= tiles * static_cast<uint32_t>(p.splits)) {
+            i -= tiles * static_cast<uint32_t>(p.splits);
+            from = tiles;
+            tiles = p.n_tiles - tiles;
+        }
+        part = static_cast<int>(i / tiles);
+        tile = static_cast<int>(from + i - part * tiles);
+    }
 };
 
 // A tile of R rows of one sequence, and the part of the sequence it is met with.
@@ -52,37 +72,47 @@ struct Tile {
     int row0;                                             // first row of the tile
     int pos0;                                             // position of the first new token
     int end;                                              // tokens that the tile's last row sees
-    int steps, parts;
+    int steps, span, parts;                               // of kStep tokens: in all, in a part
 };
 
-// Tile w: sequence s has the tiles floor(q_start[s] qpk / R) + s onwards, one number at most unused.  Every lane probes one sequence a
-// round (64 sequences: one round).  Device values are brought into range, so that whatever they hold, only rows of q and out are touched.
+// Tile w of a launch: the first R rows of sequence w, or, from w = n_seqs on, further ones: sequence s has the numbers n_seqs + floor(q_start[s] qpk /
+// R) onwards for them, as many as it can need; every lane probes one sequence a round (64 sequences: one round).  Device values are brought into range, so that whatever they hold, only rows of q and out are touched.
 template <int R>
 __device__ __forceinline__ bool find_tile(const AttendParams& p, int w, Tile& t) {
     const int lane = static_cast<int>(threadIdx.x) & 63;
     auto first = [&](int s) { return min(max(p.q_start[s], 0), p.n_new); };
-    auto base = [&](int s) { return static_cast<int64_t>(first(s)) * p.qpk / R + s; };
-    int lo = 0, hi = p.n_seqs;
-    while (hi - lo > 1) {
-        const int step = (hi - lo + 63) >> 6, s = lo + lane * step;
-        const bool at = s < hi && (lane == 0 || base(s) <= w);
-        const uint64_t m = __ballot(at);
-        lo += (63 - __builtin_clzll(m)) * step;
-        hi = min(hi, lo + step);
+    auto base = [&](int s) { return static_cast<uint32_t>(first(s) * p.qpk) / R; };
+    uint32_t tile = 0;
+    if (w < p.n_seqs) {
+        t.seq = w;
+    } else {
+        const uint32_t e = static_cast<uint32_t>(w - p.n_seqs);
+        int lo = 0, hi = p.n_seqs;
+        while (hi - lo > 1) {
+            const int step = (hi - lo + 63) >> 6, s = lo + lane * step;
+            const bool at = s < hi && (lane == 0 || base(s) <= e);
+            const uint64_t m = __ballot(at);
+            lo += (63 - __builtin_clzll(m)) * step;
+            hi = min(hi, lo + step);
+        }
+        t.seq = __builtin_amdgcn_readfirstlane(lo);
+        const uint32_t from = base(t.seq);
+        if (e < from) return false;
+        tile = e - from + 1;
     }
-    t.seq = __builtin_amdgcn_readfirstlane(lo);
     t.start = first(t.seq);
     const int n = max(first(t.seq + 1) - t.start, 0);
     t.rows = n * p.qpk;
-    const int64_t tile = w - base(t.seq);
-    if (tile < 0 || tile * R >= t.rows) return false;
+    if (tile * R >= static_cast<uint32_t>(t.rows)) return false;
     t.row0 = static_cast<int>(tile) * R;
-    const int64_t room = static_cast<int64_t>(p.pages_per_seq) << p.page_shift;
-    const int len = static_cast<int>(min(static_cast<int64_t>(max(p.kv_len[t.seq], 0)), room));
+    const int room = p.pages_per_seq << p.page_shift;
+    const int len = min(max(p.kv_len[t.seq], 0), room);
     t.pos0 = len - n;
     t.end = min(max(t.pos0 + (min(t.row0 + R, t.rows) - 1) / p.qpk + 1, 0), len);
     t.steps = (t.end + kStep - 1) / kStep;
-    t.parts = min(max(t.steps / p.least, 1), p.splits);
+    t.span = p.span;
+    if (t.steps > p.span * p.splits) t.span = (t.steps + p.splits - 1) / p.splits;
+    t.parts = max((t.steps + t.span - 1) / t.span, 1);
     return true;
 }
 
@@ -100,39 +130,53 @@ struct Bias {
 
 __device__ __forceinline__ uint32_t shifted(uint32_t x, int left) { return left >= 0 ? x << left : x >> -left; }
 
-// Two codes of `x` (halves), at bit b of each half (2 and 4 bits), as bias + code.
+// The constants of the unpacking, one and the other in registers, so that masking and placing is one operation.
+struct Places {
+    uint32_t mask, bias;
+};
 template <int BITS>
-__device__ __forceinline__ uint32_t code_pair(uint32_t x, int b) {
+__device__ __forceinline__ Places places() {
     constexpr int at = BITS == 2 ? 6 : 4;
-    constexpr uint32_t mask = ((1u << BITS) - 1u) << at;
-    return (shifted(x, at - b) & (mask | (mask << 16))) | Bias<BITS>::bits;
+    Places c{(((1u << BITS) - 1u) << at) * 0x10001u, Bias<BITS>::bits};
+    asm("" : "+s"(c.mask));
+    asm("" : "+v"(c.bias));
+    return c;
 }
 
-// 8 channels of a key, in the order in which Queries holds the query's: 0 4 1 5 2 6 3 7 (8 bits: as they come).
+// Two codes of `x` (halves), at bit b of each half (2 and 4 bits), as bias + code.
 template <int BITS>
-struct KeyWord;
+__device__ __forceinline__ uint32_t code_pair(uint32_t x, int b, const Places& c) {
+    return (shifted(x, (BITS == 2 ? 6 : 4) - b) & c.mask) | c.bias;
+}
+
+// 32 channels of a key, the lane's quarter h, and 8 of them as an operand (step s), as bias + code.  `channel`: which of the 32 the
+// operand's element e is; the queries are held in that order.
+template <int BITS>
+struct KeyWords;
 template <>
-struct KeyWord<2> {
-    uint32_t w;                                           // 16 channels, of which the lane's are the half h & 1
-    __device__ __forceinline__ void load(const unsigned char* row, int s, int h) { w = *reinterpret_cast<const uint32_t*>(row + 8 * s + 4 * (h >> 1)); }
-    __device__ __forceinline__ u32x4 pairs(int h) const {
-        const uint32_t x = byte_perm(0u, w, (h & 1) ? 0x0C030C02u : 0x0C010C00u);
-        return u32x4{code_pair<2>(x, 0), code_pair<2>(x, 2), code_pair<2>(x, 4), code_pair<2>(x, 6)};
-    }
-};
-template <>
-struct KeyWord<4> {
-    uint32_t w;
-    __device__ __forceinline__ void load(const unsigned char* row, int s, int h) { w = *reinterpret_cast<const uint32_t*>(row + 16 * s + 4 * h); }
-    __device__ __forceinline__ u32x4 pairs(int) const { return u32x4{code_pair<4>(w, 0), code_pair<4>(w, 4), code_pair<4>(w, 8), code_pair<4>(w, 12)}; }
-};
-template <>
-struct KeyWord<8> {
+struct KeyWords<2> {
     u32x2 w;
-    __device__ __forceinline__ void load(const unsigned char* row, int s, int h) { w = *reinterpret_cast<const u32x2*>(row + 32 * s + 8 * h); }
-    __device__ __forceinline__ u32x4 pairs(int) const {
-        return u32x4{byte_perm(0x64646464u, w[0], 0x04010400u), byte_perm(0x64646464u, w[0], 0x04030402u),
-                     byte_perm(0x64646464u, w[1], 0x04010400u), byte_perm(0x64646464u, w[1], 0x04030402u)};
+    static __device__ __forceinline__ constexpr int channel(int s, int e) { return 16 * (s >> 1) + 4 * (s & 1) + (e >> 1) + 8 * (e & 1); }
+    __device__ __forceinline__ void load(const unsigned char* p) { w = *reinterpret_cast<const u32x2*>(p); }
+    __device__ __forceinline__ uint32_t pair(int s, int r, const Places& c) const { return code_pair<2>(w[s >> 1], 8 * (s & 1) + 2 * r, c); }
+};
+template <>
+struct KeyWords<4> {
+    u32x4 w;
+    static __device__ __forceinline__ constexpr int channel(int s, int e) { return 8 * s + (e >> 1) + 4 * (e & 1); }
+    __device__ __forceinline__ void load(const unsigned char* p) { w = *reinterpret_cast<const u32x4*>(p); }
+    __device__ __forceinline__ uint32_t pair(int s, int r, const Places& c) const { return code_pair<4>(w[s], 4 * r, c); }
+};
+template <>
+struct KeyWords<8> {
+    u32x4 w[2];
+    static __device__ __forceinline__ constexpr int channel(int s, int e) { return 8 * s + e; }
+    __device__ __forceinline__ void load(const unsigned char* p) {
+        w[0] = *reinterpret_cast<const u32x4*>(p);
+        w[1] = *reinterpret_cast<const u32x4*>(p + 16);
+    }
+    __device__ __forceinline__ uint32_t pair(int s, int r, const Places& c) const {
+        return byte_perm(c.bias, w[s >> 1][2 * (s & 1) + (r >> 1)], (r & 1) ? 0x05030502u : 0x05010500u);
     }
 };
 
@@ -140,51 +184,219 @@ struct KeyWord<8> {
 template <int BITS>
 struct ValueWord {
     typename std::conditional<BITS == 8, u32x2, typename std::conditional<BITS == 4, uint32_t, uint16_t>::type>::type w;
-    __device__ __forceinline__ void load(const unsigned char* row, int m) { w = *reinterpret_cast<const decltype(w)*>(row + m * BITS); }
 };
 
 // Channel j of two tokens, as bias + code.
 template <int BITS>
-__device__ __forceinline__ uint32_t value_pair(const ValueWord<BITS>& a, const ValueWord<BITS>& b, int j) {
+__device__ __forceinline__ uint32_t value_pair(const ValueWord<BITS>& a, const ValueWord<BITS>& b, int j, const Places& c) {
     if constexpr (BITS == 2) {
-        return code_pair<2>(static_cast<uint32_t>(a.w) | (static_cast<uint32_t>(b.w) << 16), 2 * j);
+        return code_pair<2>(static_cast<uint32_t>(a.w) | (static_cast<uint32_t>(b.w) << 16), 2 * j, c);
     } else if constexpr (BITS == 4) {
-        return code_pair<4>(byte_perm(b.w, a.w, j < 4 ? 0x05040100u : 0x07060302u), 4 * (j & 3));
+        return code_pair<4>(byte_perm(b.w, a.w, j < 4 ? 0x05040100u : 0x07060302u), 4 * (j & 3), c);
     } else {
-        const uint32_t c = static_cast<uint32_t>(j & 3);
-        return byte_perm(b.w[j >> 2], a.w[j >> 2], 0x0C000C00u | c | ((c + 4u) << 16)) | Bias<8>::bits;
+        const uint32_t k = static_cast<uint32_t>(j & 3);
+        return byte_perm(b.w[j >> 2], a.w[j >> 2], 0x0C000C00u | k | ((k + 4u) << 16)) | c.bias;
     }
 }
 
-template <int BITS, int NG>
-struct StepLoads {
-    KeyWord<BITS> k[2][4];
-    uint32_t km[2][4][NG];
-    ValueWord<BITS> v[2][4];
-    uint32_t vm[2][4];
+__device__ __forceinline__ bool not_finite(uint32_t meta) { return (meta & 0x7C00u) == 0x7C00u || (meta & 0x7C000000u) == 0x7C000000u; }
+
+// Where a step's halves of 16 tokens lie: their first rows, and the first of their tokens that nobody sees.  A half past the end is read in the
+// last page, one in a page that does not exist in the first (and all its tokens are unseen).
+struct Pages {
+    int id[2];
 };
+struct Place {
+    uint64_t rows[2];
+    int limit[2];
+};
+struct Walk {
+    const int32_t* list;
+    int shift, offset_mask, last_page, end;
+    uint32_t n_pages, n_kv, kvh;
+    __device__ __forceinline__ Walk(const AttendParams& p, const Tile& t, int head)
+        : list(p.pages + t.seq * p.page_stride), shift(p.page_shift), offset_mask((1 << p.page_shift) - 1),
+          last_page(max(t.end - 1, 0) >> p.page_shift), end(t.end), n_pages(p.n_pages), n_kv(p.n_kv), kvh(head) {}
+    __device__ __forceinline__ Pages pages(int step) const {
+        Pages a;
+        a.id[0] = list[min(step * kStep >> shift, last_page)];
+        a.id[1] = list[min((step * kStep + 16) >> shift, last_page)];
+        return a;
+    }
+    __device__ __forceinline__ Place place(int step, const Pages& pages) const {
+        Place a;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const bool ok = static_cast<uint32_t>(pages.id[u]) < n_pages;
+            const uint32_t page = ok ? static_cast<uint32_t>(pages.id[u]) : 0u;
+            a.limit[u] = ok ? end : 0;
+            a.rows[u] = ((static_cast<uint64_t>(page) * n_kv + kvh) << shift) + static_cast<uint32_t>((step * kStep + 16 * u) & offset_mask);
+        }
+        return a;
+    }
+};
+
+// x of the lane that lies N further in the lane's sixteen.
+template <int N>
+__device__ __forceinline__ float rotated(float x) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x120 + N, 0xF, 0xF, true));
+}
+
+__device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+
+// A lane's 32 channels of a query as operands, in KeyWords' order, times a power of two that brings the row's largest element into [1/2, 1);
+// `scale`: what turns the row's products into powers of two; `sum`: the operands' sum.  `keep`: whether they count (else 0); rows that are
+// not live are 0 too.  (Elements below 2^-14 of the largest lose bits to fp16's range: 2^-25 of it at most.)
+template <int BITS, int QDT>
+__device__ __forceinline__ void load_query(const AttendParams& p, const unsigned char* src, bool live, bool keep, half8 (&qf)[4], float& scale, float& sum) {
+    u32x4 raw[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) raw[s] = *reinterpret_cast<const u32x4*>(src + 16 * s);
+    // the largest magnitude, as bits: those of both formats are ordered like their values
+    uint32_t big = 0u;
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) big = max_halves(big, raw[s][e] & 0x7FFF7FFFu);
+    big = max(big & 0xFFFFu, big >> 16);
+    big = max(big, static_cast<uint32_t>(__shfl_xor(static_cast<int>(big), 16, 64)));
+    big = max(big, static_cast<uint32_t>(__shfl_xor(static_cast<int>(big), 32, 64)));
+    const float top = QDT == SQUAT_BF16 ? as_f32(big << 16) : half_lo(big);
+    int e2 = 0;
+    if (top > 0.0f && top < INFINITY) (void)frexpf(top, &e2);
+    e2 = max(-100, min(100, e2));
+    const float factor = ldexpf(live && keep ? (p.scale < 0.0f ? -1.0f : 1.0f) : 0.0f, -e2);
+    scale = fmaxf(ldexpf(fabsf(p.scale), e2), 1e-30f);
+    sum = 0.0f;
+    if (!(live && keep)) {                                // (not by a product: what another group holds need not be finite)
+#pragma unroll
+        for (int s = 0; s < 4; ++s) raw[s] = u32x4{0u, 0u, 0u, 0u};
+    }
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int c = KeyWords<BITS>::channel(s, e);
+            const uint32_t u = raw[c >> 3][(c >> 1) & 3];
+            const float x = QDT == SQUAT_BF16 ? as_f32((c & 1) ? (u & 0xFFFF0000u) : (u << 16)) : ((c & 1) ? half_hi(u) : half_lo(u));
+            qf[s][e] = static_cast<_Float16>(x * factor);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            sum = __builtin_amdgcn_fdot2(half2v{qf[s][2 * e], qf[s][2 * e + 1]}, half2v{static_cast<_Float16>(1.0f), static_cast<_Float16>(1.0f)}, sum, false);
+    }
+}
+
+// Row r of a tile from the wavefronts' sums (16 threads, 8 channels each; at: the row's place in `sums`): to the result or to the part's place.
+template <int R, int QDT, int N>
+__device__ __forceinline__ void finish_row(const AttendParams& p, const Tile& t, const Work& work, int r, const float (&sums)[kWaves][N][kPitch],
+                                           const float2 (&stats)[kWaves][R], int at) {
+    const int c0 = (static_cast<int>(threadIdx.x) & 15) * 8;
+    const int row = t.row0 + r;
+    if (row >= t.rows) return;
+    float all = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) all = fmaxf(all, stats[w][r].x);
+    float sum = 0.0f, acc[8];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) acc[c] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        const float2 st = stats[w][r];
+        const float by = st.x > -INFINITY ? __builtin_amdgcn_exp2f(st.x - all) : 1.0f;
+        sum += by * st.y;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) acc[c] = fmaf(by, sums[w][at][c0 + c], acc[c]);
+    }
+    if (p.splits > 1) {
+        const int64_t to_row = ((static_cast<int64_t>(work.part) * p.n_tiles + work.tile) * p.n_kv + work.kvh) * R + r;
+        float* to = p.part_o + to_row * kD + c0;
+        *reinterpret_cast<f32x4*>(to) = f32x4{acc[0], acc[1], acc[2], acc[3]};
+        *reinterpret_cast<f32x4*>(to + 4) = f32x4{acc[4], acc[5], acc[6], acc[7]};
+        if (c0 == 0) p.part_ml[to_row] = float2{all, sum};
+        return;
+    }
+    const int i = row / p.qpk, hq = work.kvh * p.qpk + (row - i * p.qpk);
+    const float by = sum == 0.0f ? 1.0f : 1.0f / sum;
+    unsigned char* to = p.out + ((t.start + i) * p.ost + hq * p.osh + c0) * 2;
+    if constexpr (QDT == SQUAT_BF16) {
+        bf16x8 v;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) v[c] = static_cast<__bf16>(acc[c] * by);
+        *reinterpret_cast<bf16x8*>(to) = v;
+    } else {
+        half8 v;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) v[c] = static_cast<_Float16>(acc[c] * by);
+        *reinterpret_cast<half8*>(to) = v;
+    }
+    if (p.lse && c0 == 0)
+        p.lse[static_cast<int64_t>(t.start + i) * p.n_kv * p.qpk + hq] = sum == 0.0f ? -INFINITY : kLn2 * ((all - kLift) + __builtin_amdgcn_logf(sum));
+}
 
 template <int BITS, int NG, int NQ, int QDT>
 __global__ void __launch_bounds__(256) attend_kernel(const AttendParams p) {
     constexpr int R = 16 * NQ;
     constexpr int ROW = kD * BITS / 8;                    // bytes of a token's codes
-    constexpr bool SPLIT_P = QDT == SQUAT_F16;            // weights as high and low fp16 parts (the fp16 result has 3 bits more than bf16's)
+    constexpr int MROW = 4 * NG;                          // of its scales and zero-points
+    // An fp16 result has three bits more than bf16's: weights as high and low fp16 parts.
+    constexpr bool SPLIT_P = QDT == SQUAT_F16;
     __shared__ float sums[kWaves][16][kPitch];
     __shared__ float2 stats[kWaves][R];
-    const int bx = static_cast<int>(blockIdx.x), w_tile = bx / p.n_kv, kvh = bx - w_tile * p.n_kv;
+    const Work work(p);
+    const int part = work.part, kvh = work.kvh;
     Tile t;
-    if (!find_tile<R>(p, w_tile, t)) return;
-    const int part = static_cast<int>(blockIdx.y);
-    if (part >= t.parts) return;
+    if (!find_tile<R>(p, work.tile, t) || part >= t.parts) return;
     const int lane = static_cast<int>(threadIdx.x) & 63, m = lane & 15, h = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
-    const int first = static_cast<int>(static_cast<int64_t>(t.steps) * part / t.parts);
-    const int last = static_cast<int>(static_cast<int64_t>(t.steps) * (part + 1) / t.parts);
+    const int first = part * t.span, last = min(first + t.span, t.steps);
 
-    // The queries, as operands: step s is channels 32 s to 32 s + 31, a lane's are 8 of them from 32 s + 8 h on, in KeyWord's order.
-    half8 qf[NQ][4];
-    f32x4 start[NQ][NG];                                  // -bias * sum of a group's queries
-    float qs[NQ][NG], scale[NQ];
+    const Walk walk(p, t, kvh);
+    // A step's loads.  Keys: the quarter h of lane m's token, and its group's scale and zero-point.  Values: 8 channels from 8 m on of
+    // the tokens 4 h + i, and their group's.
+    KeyWords<BITS> kw[2];
+    uint32_t km[2];
+    ValueWord<BITS> vw[2][4];
+    uint32_t vm[2][4];
+    const uint32_t k_at = m * ROW + h * (ROW / 4), v_at = 4 * h * ROW + m * BITS;
+    const uint32_t km_at = m * MROW + 4 * ((h * NG) >> 2), vm_at = 4 * h * MROW + 4 * ((m * NG) >> 4);
+    auto load_keys = [&](const Place& a) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const unsigned char *codes = p.kc + a.rows[u] * ROW, *meta = p.km + a.rows[u] * MROW;
+            kw[u].load(codes + k_at);
+            km[u] = *reinterpret_cast<const uint32_t*>(meta + km_at);
+        }
+    };
+    auto load_values = [&](const Place& a) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const unsigned char *codes = p.vc + a.rows[u] * ROW, *meta = p.vm + a.rows[u] * MROW;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                vw[u][i].w = *reinterpret_cast<const decltype(vw[u][i].w)*>(codes + v_at + i * ROW);
+                vm[u][i] = *reinterpret_cast<const uint32_t*>(meta + vm_at + i * MROW);
+            }
+        }
+    };
+
+    int step = first + wave;
+    Place at;
+    Pages ahead;
+    if (step < last) {                                    // uniform
+        at = walk.place(step, walk.pages(step));
+        load_keys(at);
+        load_values(at);
+        ahead = walk.pages(step + kWaves);                  // (past the end: the last page's)
+    }
+
+    // The queries, as operands: a lane's are the 32 channels of its quarter h, 8 a step.  qz: what the zero-points meet, the sum of the
+    // quarter's queries as a high and a low part.
+    half8 qf[NQ][4], qz[NQ];
+    float scale[NQ], slack[NQ];                           // of a row's raw logits, to powers of two; kSlack in raw logits
     int seen[NQ];                                         // the last token that the lane's row sees
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
@@ -193,171 +405,114 @@ __global__ void __launch_bounds__(256) attend_kernel(const AttendParams p) {
         const int r = live ? row : t.rows - 1;
         const int i = r / p.qpk, hq = kvh * p.qpk + (r - i * p.qpk);
         seen[n] = live ? t.pos0 + i : -1;
-        const unsigned char* src = p.q + ((t.start + i) * p.qst + hq * p.qsh + 8 * h) * 2;
-        float sum[4], top = 0.0f;
-        u32x4 raw[4];
+        float sum;
+        load_query<BITS, QDT>(p, p.q + ((t.start + i) * p.qst + hq * p.qsh + 32 * h) * 2, live, true, qf[n], scale[n], sum);
+        slack[n] = kSlack / scale[n];
 #pragma unroll
-        for (int s = 0; s < 4; ++s) raw[s] = *reinterpret_cast<const u32x4*>(src + 64 * s);
-        float factor = 1.0f;
-        if constexpr (QDT == SQUAT_BF16) {                // by a power of two into [1/2, 1): exact, and whatever the row's size
-#pragma unroll
-            for (int s = 0; s < 4; ++s)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) top = fmaxf(top, fmaxf(fabsf(as_f32(raw[s][e] << 16)), fabsf(as_f32(raw[s][e] & 0xFFFF0000u))));
-            top = fmaxf(top, __shfl_xor(top, 16, 64));
-            top = fmaxf(top, __shfl_xor(top, 32, 64));
-            int e = 0;
-            if (top > 0.0f && top < INFINITY) (void)frexpf(top, &e);
-            e = max(-100, min(100, e));
-            factor = ldexpf(1.0f, -e);
-            scale[n] = ldexpf(p.scale, e);
-        } else {
-            scale[n] = p.scale;
-        }
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            _Float16 c[8];
-            sum[s] = 0.0f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t u = raw[s][e >> 1];
-                if constexpr (QDT == SQUAT_BF16) c[e] = static_cast<_Float16>(as_f32((e & 1) ? (u & 0xFFFF0000u) : (u << 16)) * factor);
-                else c[e] = as_half2(u)[e & 1];
-                if (!live) c[e] = static_cast<_Float16>(0.0f);
-                sum[s] += static_cast<float>(c[e]);
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) qf[n][s][e] = BITS == 8 ? c[e] : c[(e >> 1) + 4 * (e & 1)];
-            sum[s] += __shfl_xor(sum[s], 16, 64);
-            sum[s] += __shfl_xor(sum[s], 32, 64);
-        }
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            qs[n][g] = 0.0f;
-#pragma unroll
-            for (int s = 0; s < 4 / NG; ++s) qs[n][g] += sum[g * (4 / NG) + s];
-            const float b = -Bias<BITS>::value * qs[n][g];
-            start[n][g] = f32x4{b, b, b, b};
-        }
+        for (int e = 0; e < 8; ++e) qz[n][e] = static_cast<_Float16>(0.0f);
+        qz[n][0] = static_cast<_Float16>(sum);
+        qz[n][1] = static_cast<_Float16>(sum - static_cast<float>(qz[n][0]));
     }
     const int least_seen = t.pos0 + t.row0 / p.qpk;       // every live row sees this token and all before it
+    const Places places_ = places<BITS>();
+    const half2v bias = {static_cast<_Float16>(Bias<BITS>::value), static_cast<_Float16>(Bias<BITS>::value)};
 
-    f32x4 o[NQ][8];                                       // O^T: channels 8 (4 h + i) + j, column m
-    float top[NQ], total[NQ];
+    f32x4 o[NQ][8], total[NQ];                            // O^T: channels 8 (4 h + i) + j, column m; the weights' sum
+    float top[NQ];
+    half8 ones;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ones[e] = static_cast<_Float16>(1.0f);
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
         top[n] = -INFINITY;
-        total[n] = 0.0f;
+        total[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int j = 0; j < 8; ++j) o[n][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
-    const int32_t* list = p.pages + t.seq * p.page_stride;
-    const int offset_mask = (1 << p.page_shift) - 1;
-    // Rows of a half step of 16 tokens: the page's, or, past the end or in a page that does not exist, some that do; `limit` is the first
-    // of its tokens that nobody sees.
-    auto rows_of = [&](int token, int& limit) {
-        const bool past = token >= t.end;
-        const int page = list[(past ? token - 16 : token) >> p.page_shift];
-        const bool ok = page >= 0 && page < p.n_pages && !past;
-        limit = ok ? t.end : token;
-        return ((static_cast<int64_t>(ok ? page : 0) * p.n_kv + kvh) << p.page_shift) + (token & offset_mask);
-    };
-
-    for (int step = first + wave; step < last; step += kWaves) {
+    while (step < last) {
         const int t0 = step * kStep;
-        int limit[2];
-        StepLoads<BITS, NG> in;
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int64_t rows = rows_of(t0 + 16 * u, limit[u]);
-            const unsigned char* kc = p.kc + rows * ROW + m * ROW;
-#pragma unroll
-            for (int s = 0; s < 4; ++s) in.k[u][s].load(kc, s, h);
-            const unsigned char* km = p.km + (rows + 4 * h) * (4 * NG);
-            const unsigned char* vc = p.vc + (rows + 4 * h) * ROW;
-            const unsigned char* vm = p.vm + (rows + 4 * h) * (4 * NG) + 4 * ((m * NG) >> 4);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (NG == 4) {
-                    const u32x4 x = *reinterpret_cast<const u32x4*>(km + i * 16);
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) in.km[u][i][g] = x[g];
-                } else if constexpr (NG == 2) {
-                    const u32x2 x = *reinterpret_cast<const u32x2*>(km + i * 8);
-                    in.km[u][i][0] = x[0];
-                    in.km[u][i][1] = x[1];
-                } else {
-                    in.km[u][i][0] = *reinterpret_cast<const uint32_t*>(km + i * 4);
-                }
-                in.v[u][i].load(vc + i * ROW, m);
-                in.vm[u][i] = *reinterpret_cast<const uint32_t*>(vm + i * (4 * NG));
-            }
+        const int limit0 = at.limit[0], limit1 = at.limit[1];
+        step += kWaves;
+        const bool more = step < last;
+        if (more) {
+            at = walk.place(step, ahead);
+            ahead = walk.pages(step + kWaves);
         }
 
         // logits: lane's column m, tokens t0 + 16 u + 4 h + i
         float x[NQ][2][4];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            half8 kf[4];
-#pragma unroll
-            for (int s = 0; s < 4; ++s) kf[s] = __builtin_bit_cast(half8, in.k[u][s].pairs(h));
+            const half2v sz = as_half2(km[u]), odd = sz * half2v{static_cast<_Float16>(0.0f), static_cast<_Float16>(0.0f)};
+            const _Float16 zero = sz[1] + (odd[0] + odd[1]);                  // (metadata that is not finite: NaN)
+            const half2v ks = {sz[0], sz[0]}, kz = {zero, zero};
+            f32x4 a[NQ];
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
+                a[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                const half8 zf = __builtin_bit_cast(half8, (u32x4{__builtin_bit_cast(uint32_t, kz), 0u, 0u, 0u}));
+                a[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(zf, qz[n], a[n], 0, 0, 0);
+            }
 #pragma unroll
-                for (int g = 0; g < NG; ++g) {
-                    f32x4 a = start[n][g];
+            for (int s = 0; s < 4; ++s) {
+                u32x4 hi, lo;
 #pragma unroll
-                    for (int s = 0; s < 4 / NG; ++s) a = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[g * (4 / NG) + s], qf[n][g * (4 / NG) + s], a, 0, 0, 0);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float z = half_hi(in.km[u][i][g]) * qs[n][g];
-                        x[n][u][i] = fmaf(half_lo(in.km[u][i][g]), a[i], g == 0 ? z : x[n][u][i] + z);
-                    }
+                for (int r = 0; r < 4; ++r) {
+                    const half2v c = as_half2(kw[u].pair(s, r, places_)) - bias;
+                    const half2v y = c * ks;              // code * scale without its rounding: a high and a low part
+                    hi[r] = __builtin_bit_cast(uint32_t, y);
+                    lo[r] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(c, ks, -y));
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[n][u][i] = fmaf(x[n][u][i], 0.0f, x[n][u][i]) * scale[n];       // (infinite metadata: NaN)
+                for (int n = 0; n < NQ; ++n) {
+                    a[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, hi), qf[n][s], a[n], 0, 0, 0);
+                    a[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, lo), qf[n][s], a[n], 0, 0, 0);
+                }
             }
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[n][u][i] = a[n][i];
         }
+        if (more) load_keys(at);                          // (in flight behind the values', which come back first)
+
         // the last tokens, the ones that not every row sees, and pages that do not exist
-        const bool edge = t0 + kStep > least_seen + 1 || t0 + 16 > limit[0] || t0 + kStep > limit[1];       // uniform
+        const bool edge = t0 + kStep > least_seen + 1 || t0 + 16 > limit0 || t0 + kStep > limit1;       // uniform
         if (edge) {
+            bool odd = false;
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int token = t0 + 16 * u + 4 * h + i;
-                    const bool there = token < limit[u];
-                    if (!there) in.vm[u][i] = 0u;         // (whatever the page holds behind the last token)
+                    const bool there = token < (u ? limit1 : limit0);
+                    if (!there) vm[u][i] = 0u;            // (whatever the page holds behind the last token)
 #pragma unroll
                     for (int n = 0; n < NQ; ++n)
                         if (!there || token > seen[n]) x[n][u][i] = -INFINITY;
+                    odd |= not_finite(vm[u][i]);
                 }
             // A token that only some rows see spoils those alone: NaN and infinity would reach the others as 0 * NaN.
-            bool odd = false;
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    odd |= (in.vm[u][i] & 0x7C00u) == 0x7C00u || (in.vm[u][i] & 0x7C000000u) == 0x7C000000u;
             if (__ballot(odd)) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if ((in.vm[u][i] & 0x7C00u) == 0x7C00u || (in.vm[u][i] & 0x7C000000u) == 0x7C000000u) in.vm[u][i] = 0u;
+                        if (not_finite(vm[u][i])) vm[u][i] = 0u;
                 // this lane's sums are of the channels 32 h to 32 h + 31
+                const Place here = walk.place(t0 / kStep, walk.pages(t0 / kStep));
+#pragma unroll 1
                 for (int k = 0; k < kStep; ++k) {
-                    int lim;
-                    const int64_t rows = rows_of(t0 + (k & 16), lim);
-                    if (t0 + k >= lim) continue;
-                    const uint32_t meta = *reinterpret_cast<const uint32_t*>(p.vm + (rows + (k & 15)) * (4 * NG) + 4 * ((h * NG) >> 2));
-                    const bool spoilt = (meta & 0x7C00u) == 0x7C00u || (meta & 0x7C000000u) == 0x7C000000u;
+                    if (t0 + k >= (k < 16 ? here.limit[0] : here.limit[1])) continue;
+                    const uint64_t row = (k < 16 ? here.rows[0] : here.rows[1]) + (k & 15);
+                    const uint32_t meta = *reinterpret_cast<const uint32_t*>(p.vm + row * MROW + 4 * ((h * NG) >> 2));
 #pragma unroll
-                    for (int n = 0; n < NQ; ++n)
-                        if (spoilt && t0 + k <= seen[n])
+                    for (int n = 0; n < NQ; ++n) {
+                        const float add = not_finite(meta) && t0 + k <= seen[n] ? NAN : 0.0f;
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) o[n][j] += NAN;
+                        for (int j = 0; j < 8; ++j) o[n][j] += add;
+                    }
                 }
             }
         }
@@ -369,31 +524,32 @@ __global__ void __launch_bounds__(256) attend_kernel(const AttendParams p) {
             float most = x[n][0][0];
 #pragma unroll
             for (int e = 1; e < 8; ++e) most = fmaxf(most, x[n][e >> 2][e & 3]);
-            if (__ballot(most > top[n] + kSlack)) {
+            if (__ballot(most > top[n] + slack[n])) {
                 most = fmaxf(most, __shfl_xor(most, 16, 64));
                 most = fmaxf(most, __shfl_xor(most, 32, 64));
                 const float now = fmaxf(top[n], most);
-                const float by = now > -INFINITY ? __builtin_amdgcn_exp2f(top[n] - now) : 1.0f;
+                const float by = now > -INFINITY ? __builtin_amdgcn_exp2f((top[n] - now) * scale[n]) : 1.0f;
                 top[n] = now;
                 total[n] *= by;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) o[n][j] *= by;
             }
-            const float from = top[n] > -INFINITY ? top[n] - kLift : 0.0f;
+            const float from = top[n] > -INFINITY ? kLift - top[n] * scale[n] : 0.0f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float w = __builtin_amdgcn_exp2f(x[n][e >> 2][e & 3] - from);
-                total[n] += w;
+                const float w = __builtin_amdgcn_exp2f(fmaf(x[n][e >> 2][e & 3], scale[n], from));
                 pf[n][e] = static_cast<_Float16>(w);
                 if constexpr (SPLIT_P) pl[n][e] = static_cast<_Float16>(w - static_cast<float>(pf[n][e]));
             }
+            total[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pf[n], total[n], 0, 0, 0);
+            if constexpr (SPLIT_P) total[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pl[n], total[n], 0, 0, 0);
         }
 
         // values: operand j is channel 8 m + j of the tokens t0 + 4 h + i, t0 + 16 + 4 h + i
         half2v vs[4], vz[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const uint32_t a = in.vm[e >> 1][2 * (e & 1)], b = in.vm[e >> 1][2 * (e & 1) + 1];
+            const uint32_t a = vm[e >> 1][2 * (e & 1)], b = vm[e >> 1][2 * (e & 1) + 1];
             vs[e] = as_half2(byte_perm(b, a, 0x05040100u));
             vz[e] = as_half2(byte_perm(b, a, 0x07060302u));
         }
@@ -402,8 +558,7 @@ __global__ void __launch_bounds__(256) attend_kernel(const AttendParams p) {
             u32x4 raw;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const half2v c = as_half2(value_pair<BITS>(in.v[e >> 1][2 * (e & 1)], in.v[e >> 1][2 * (e & 1) + 1], j)) -
-                                 half2v{static_cast<_Float16>(Bias<BITS>::value), static_cast<_Float16>(Bias<BITS>::value)};
+                const half2v c = as_half2(value_pair<BITS>(vw[e >> 1][2 * (e & 1)], vw[e >> 1][2 * (e & 1) + 1], j, places_)) - bias;
                 raw[e] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(c, vs[e], vz[e]));
             }
             const half8 vf = __builtin_bit_cast(half8, raw);
@@ -413,14 +568,13 @@ __global__ void __launch_bounds__(256) attend_kernel(const AttendParams p) {
                 if constexpr (SPLIT_P) o[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pl[n], o[n][j], 0, 0, 0);
             }
         }
+        if (more) load_values(at);
     }
 
     // the four wavefronts' sums, 16 rows at a time
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
-        total[n] += __shfl_xor(total[n], 16, 64);
-        total[n] += __shfl_xor(total[n], 32, 64);
-        if (h == 0) stats[wave][16 * n + m] = float2{top[n], total[n]};
+        if (h == 0) stats[wave][16 * n + m] = float2{top[n] > -INFINITY ? top[n] * scale[n] : -INFINITY, total[n][0]};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             float* to = &sums[wave][m][8 * (4 * h + i)];
@@ -428,51 +582,210 @@ __global__ void __launch_bounds__(256) attend_kernel(const AttendParams p) {
             *reinterpret_cast<f32x4*>(to + 4) = f32x4{o[n][4][i], o[n][5][i], o[n][6][i], o[n][7][i]};
         }
         __syncthreads();
-        const int r = static_cast<int>(threadIdx.x) >> 4, c0 = (static_cast<int>(threadIdx.x) & 15) * 8;
-        const int row = t.row0 + 16 * n + r;
-        if (row < t.rows) {
-            float all = -INFINITY;
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) all = fmaxf(all, stats[w][16 * n + r].x);
-            float sum = 0.0f, acc[8];
-#pragma unroll
-            for (int c = 0; c < 8; ++c) acc[c] = 0.0f;
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                const float2 st = stats[w][16 * n + r];
-                const float by = st.x > -INFINITY ? __builtin_amdgcn_exp2f(st.x - all) : 1.0f;
-                sum += by * st.y;
-#pragma unroll
-                for (int c = 0; c < 8; ++c) acc[c] = fmaf(by, sums[w][r][c0 + c], acc[c]);
-            }
-            if (p.splits > 1) {
-                const int64_t at = (static_cast<int64_t>(part) * p.n_tiles * p.n_kv + bx) * R + 16 * n + r;
-                float* to = p.part_o + at * kD + c0;
-                *reinterpret_cast<f32x4*>(to) = f32x4{acc[0], acc[1], acc[2], acc[3]};
-                *reinterpret_cast<f32x4*>(to + 4) = f32x4{acc[4], acc[5], acc[6], acc[7]};
-                if (c0 == 0) p.part_ml[at] = float2{all, sum};
-            } else {
-                const int i = row / p.qpk, hq = kvh * p.qpk + (row - i * p.qpk);
-                const float by = sum == 0.0f ? 1.0f : 1.0f / sum;
-                unsigned char* to = p.out + ((t.start + i) * p.ost + hq * p.osh + c0) * 2;
-                if constexpr (QDT == SQUAT_BF16) {
-                    bf16x8 v;
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) v[c] = static_cast<__bf16>(acc[c] * by);
-                    *reinterpret_cast<bf16x8*>(to) = v;
-                } else {
-                    half8 v;
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) v[c] = static_cast<_Float16>(acc[c] * by);
-                    *reinterpret_cast<half8*>(to) = v;
-                }
-                if (p.lse && c0 == 0)
-                    p.lse[static_cast<int64_t>(t.start + i) * p.n_kv * p.qpk + hq] =
-                        sum == 0.0f ? -INFINITY : kLn2 * ((all - kLift) + __builtin_amdgcn_logf(sum));
-            }
-        }
+        const int r = static_cast<int>(threadIdx.x) >> 4;
+        finish_row<R, QDT>(p, t, work, 16 * n + r, sums, stats, r);
         if (n + 1 < NQ) __syncthreads();
     }
+}
+
+// A few rows, at most 16 / NG of a sequence and KV head (a decoded token's query heads): the matrix instructions' 16 columns hold every row
+// NG times, column n = (group g, row), so that scales need not enter the operands.
+//   Keys: column (g, row) meets the channels of group g alone (the query is 0 elsewhere), code by code; times scale[t,g], plus zero[t,g]
+//   times the sum of the group's queries, and summed over the NG columns of a row (rotations by lanes of 16).
+//   Values: column (g, row) has the weights p_t scale[t,g], which gives sum_t p_t scale[t,g] code_t for every channel; those of group g
+//   are kept.  The zero-points' part, sum_t p_t zero[t,g], is a sum in the lane.
+// Codes enter as integers, both products are exact but for the weights' rounding to fp16, and a code costs what its unpacking costs.
+// shift: a column's weights carry 2^-shift, which keeps p_t scale[t,g] below 2^(kLift + kSlack); it rises with the scales.
+template <int BITS, int NG, int QDT>
+__global__ void __launch_bounds__(256) attend_few_kernel(const AttendParams p) {
+    constexpr int R = 16 / NG;
+    constexpr int ROW = kD * BITS / 8, MROW = 4 * NG;     // bytes of a token's codes, and of its scales and zero-points
+    __shared__ float sums[kWaves][R][kPitch];
+    __shared__ float2 stats[kWaves][R];
+    const Work work(p);
+    const int part = work.part, kvh = work.kvh;
+    Tile t;
+    if (!find_tile<R>(p, work.tile, t) || part >= t.parts) return;
+    const int lane = static_cast<int>(threadIdx.x) & 63, m = lane & 15, h = lane >> 4;
+    const int g = m / R, rr = m % R;                      // the lane's column
+    const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+    const int first = part * t.span, last = min(first + t.span, t.steps);
+    const Walk walk(p, t, kvh);
+
+    // A step's loads.  Keys: the quarter h of lane m's token, and the column's group's scale and zero-point of the tokens 4 h + i.  Values: 8
+    // channels from 8 m on of the tokens 4 h + i, and the column's group's (which is those channels').
+    KeyWords<BITS> kw[2];
+    ValueWord<BITS> vw[2][4];
+    uint32_t km[2][4], vm[2][4];
+    const uint32_t k_at = m * ROW + h * (ROW / 4), v_at = 4 * h * ROW + m * BITS, m_at = 4 * h * MROW + 4 * g;
+    auto load_meta = [&](const unsigned char* from, uint32_t (&to)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to[i] = *reinterpret_cast<const uint32_t*>(from + m_at + i * MROW);
+    };
+    auto load_keys = [&](const Place& a) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            kw[u].load(p.kc + a.rows[u] * ROW + k_at);
+            load_meta(p.km + a.rows[u] * MROW, km[u]);
+        }
+    };
+    auto load_values = [&](const Place& a) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const unsigned char* codes = p.vc + a.rows[u] * ROW;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) vw[u][i].w = *reinterpret_cast<const decltype(vw[u][i].w)*>(codes + v_at + i * ROW);
+            load_meta(p.vm + a.rows[u] * MROW, vm[u]);
+        }
+    };
+    int step = first + wave;
+    Place at;
+    Pages ahead;
+    if (step < last) {                                    // uniform
+        at = walk.place(step, walk.pages(step));
+        load_keys(at);
+        load_values(at);
+        ahead = walk.pages(step + kWaves);                // (past the end: the last page's)
+    }
+
+    // The query, brought to a largest element in [1/2, 1) by a power of two; of the column's group only.
+    const int row = t.row0 + rr;
+    const bool live = row < t.rows;
+    const int qi = (live ? row : t.rows - 1) / p.qpk, hq = kvh * p.qpk + (live ? row : t.rows - 1) - qi * p.qpk;
+    const int seen = live ? t.pos0 + qi : -1;             // the last token that the row sees
+    half8 qf[4];
+    float scale, group_sum;
+    load_query<BITS, QDT>(p, p.q + ((t.start + qi) * p.qst + hq * p.qsh + 32 * h) * 2, live, (h * NG) >> 2 == g, qf, scale, group_sum);
+    group_sum += __shfl_xor(group_sum, 16, 64);
+    group_sum += __shfl_xor(group_sum, 32, 64);
+    const float slack = kSlack / scale, neg = -Bias<BITS>::value * group_sum;
+    const f32x4 start = {neg, neg, neg, neg};
+    const int least_seen = t.pos0 + t.row0 / p.qpk;       // every live row sees this token and all before it
+    const Places places_ = places<BITS>();
+    const half2v zero2 = {static_cast<_Float16>(0.0f), static_cast<_Float16>(0.0f)};
+
+    f32x4 o[8], weight = {0.0f, 0.0f, 0.0f, 0.0f};        // O^T: channels 8 (4 h + i) + j; the sum of p scale
+    float top = -INFINITY, total = 0.0f, zeros = 0.0f;    // total: sum of p; zeros: sum of p zero (the lane's tokens)
+    int shift = -15;
+    half8 ones;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ones[e] = static_cast<_Float16>(1.0f);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    while (step < last) {
+        const int t0 = step * kStep;
+        const int limit0 = at.limit[0], limit1 = at.limit[1];
+        step += kWaves;
+        const bool more = step < last;
+        if (more) {
+            at = walk.place(step, ahead);
+            ahead = walk.pages(step + kWaves);
+        }
+
+        // logits: the tokens t0 + 16 u + 4 h + i
+        float x[2][4];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            f32x4 a = start;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                u32x4 c;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) c[r] = kw[u].pair(s, r, places_);
+                a = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, c), qf[s], a, 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                // (0 scale + 0 zero: NaN where one of them is not finite)
+                float y = fmaf(half_hi(km[u][i]), group_sum, __builtin_amdgcn_fdot2(as_half2(km[u][i]), zero2, 0.0f, false));
+                y = fmaf(half_lo(km[u][i]), a[i], y);
+                if constexpr (NG >= 2) y += rotated<8>(y);
+                if constexpr (NG >= 4) y += rotated<4>(y);
+                x[u][i] = y;
+            }
+        }
+        if (more) load_keys(at);                          // (in flight behind the values', which come back first)
+
+        // the last tokens, the ones that not every row sees, and pages that do not exist
+        const bool edge = t0 + kStep > least_seen + 1 || t0 + 16 > limit0 || t0 + kStep > limit1;       // uniform
+        if (edge) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int token = t0 + 16 * u + 4 * h + i;
+                    if (token < (u ? limit1 : limit0) && token <= seen) continue;
+                    x[u][i] = -INFINITY;
+                    vm[u][i] = 0u;                        // whatever the page holds there: NaN and infinity are in the scales alone
+                }
+        }
+
+        // weights
+        float most = x[0][0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) most = fmaxf(most, x[e >> 2][e & 3]);
+        uint32_t wide = vm[0][0];                         // the largest scale, as bits (scales are not negative), in the low half
+#pragma unroll
+        for (int e = 1; e < 8; ++e) wide = max_halves(wide, vm[e >> 2][e & 3]);
+        wide &= 0x7FFFu;
+        if (__ballot(most > top + slack || static_cast<int>(wide >> 10) - 14 > shift)) {
+            most = fmaxf(most, __shfl_xor(most, 16, 64));
+            most = fmaxf(most, __shfl_xor(most, 32, 64));
+            int up = static_cast<int>(wide >> 10) - 14;   // scales are below 2^up
+            up = max(up, __shfl_xor(up, 16, 64));
+            up = max(max(up, __shfl_xor(up, 32, 64)), shift);
+            const float now = fmaxf(top, most);
+            const float by = now > -INFINITY ? __builtin_amdgcn_exp2f((top - now) * scale + static_cast<float>(shift - up)) : 1.0f;
+            top = now;
+            shift = up;
+            total *= by;
+            zeros *= by;
+            weight *= by;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] *= by;
+        }
+        const float from = top > -INFINITY ? kLift - static_cast<float>(shift) - top * scale : 0.0f;
+        half8 pf;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t sz = vm[e >> 2][e & 3];
+            const float w = __builtin_amdgcn_exp2f(fmaf(x[e >> 2][e & 3], scale, from));
+            total += w;
+            zeros = fmaf(half_hi(sz), w, zeros);
+            pf[e] = static_cast<_Float16>(half_lo(sz) * w);
+        }
+        weight = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pf, weight, 0, 0, 0);
+
+        // values: operand j is channel 8 m + j of the tokens t0 + 4 h + i, t0 + 16 + 4 h + i
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            u32x4 c;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) c[e] = value_pair<BITS>(vw[e >> 1][2 * (e & 1)], vw[e >> 1][2 * (e & 1) + 1], j, places_);
+            o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, c), pf, o[j], 0, 0, 0);
+        }
+        if (more) load_values(at);
+    }
+
+    // The four wavefronts' sums.  A lane has its column's group where its channels, 32 h to 32 h + 31, are of that group.
+    total += __shfl_xor(total, 16, 64);
+    total += __shfl_xor(total, 32, 64);
+    zeros += __shfl_xor(zeros, 16, 64);
+    zeros += __shfl_xor(zeros, 32, 64);
+    const float back = ldexpf(1.0f, shift), add = fmaf(-Bias<BITS>::value, weight[0], zeros);
+    if (h == 0 && g == 0) stats[wave][rr] = float2{top > -INFINITY ? top * scale : -INFINITY, total * back};
+    if ((h * NG) >> 2 == g) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float* to = &sums[wave][rr][32 * h + 8 * i];
+            *reinterpret_cast<f32x4*>(to) = f32x4{o[0][i] + add, o[1][i] + add, o[2][i] + add, o[3][i] + add} * back;
+            *reinterpret_cast<f32x4*>(to + 4) = f32x4{o[4][i] + add, o[5][i] + add, o[6][i] + add, o[7][i] + add} * back;
+        }
+    }
+    __syncthreads();
+    const int r = static_cast<int>(threadIdx.x) >> 4;
+    if (r < R) finish_row<R, QDT>(p, t, work, r, sums, stats, r);
 }
 
 // The parts of a row put together: one workgroup a row, a wavefront every fourth part, two channels a lane.
@@ -529,9 +842,9 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const AttendParams p) 
 }
 
 struct Plan {
-    int nq;                                               // row tiles of 16 nq rows
+    int nq, rows;                                         // row tiles: of 16 nq rows, or (nq = 0) of a few
     int64_t tiles;
-    int splits, least;
+    int splits, span;
     size_t o_bytes, ml_bytes;
 };
 
@@ -542,19 +855,24 @@ Plan plan_attend(const squat_paged_store* s, int n_seqs, int64_t n_new, int q_pe
     const int64_t room = static_cast<int64_t>(pages_per_seq) * s->page_tokens;
     if (max_new < 1 || max_new > n_new) max_new = n_new;
     if (max_kv < 1 || max_kv > room) max_kv = room;
-    a.nq = max_new * q_per_kv <= 16 ? 1 : 2;
-    const int64_t rows = 16 * a.nq;
-    a.tiles = n_new * q_per_kv / rows + n_seqs;
+    const int few = s->group / 8;                         // 16 columns, 128 / group of them a row
+    a.nq = max_new * q_per_kv <= few ? 0 : max_new * q_per_kv <= 16 ? 1 : 2;
+    a.rows = a.nq == 0 ? few : 16 * a.nq;
+    a.tiles = n_new * q_per_kv / a.rows + n_seqs;
     // tiles with work: what the hints allow
-    int64_t busy = n_seqs * ((max_new * q_per_kv + rows - 1) / rows);
+    int64_t busy = n_seqs * ((max_new * q_per_kv + a.rows - 1) / a.rows);
     busy = (busy < a.tiles ? busy : a.tiles) * s->n_kv_heads;
-    a.least = 4;
-    const int64_t wanted = (4 * device_cu_count() + busy - 1) / busy;
-    const int64_t most = (max_kv + kStep * a.least - 1) / (kStep * a.least);
-    int64_t n = wanted < most ? wanted : most;
+    const int64_t steps = (max_kv + kStep - 1) / kStep, wanted = (kTarget * device_cu_count() + busy - 1) / busy;
+    int64_t span = (steps + wanted - 1) / wanted;
+    span = span < kLeast ? kLeast : span;
+    int64_t n = (steps + span - 1) / span;
     n = n > 256 ? 256 : n;
+    const int64_t room_for = 0x7FFFFFFF / (a.tiles * s->n_kv_heads);        // (one dimension of workgroups)
+    n = n > room_for ? room_for : n;
     a.splits = n < 1 ? 1 : static_cast<int>(n);
-    const size_t all = a.splits > 1 ? static_cast<size_t>(a.splits) * a.tiles * s->n_kv_heads * rows : 0;
+    a.span = static_cast<int>((steps + a.splits - 1) / a.splits);
+    a.span = a.span < 1 ? 1 : a.span;
+    const size_t all = a.splits > 1 ? static_cast<size_t>(a.splits) * a.tiles * s->n_kv_heads * a.rows : 0;
     a.o_bytes = up256(all * kD * sizeof(float));
     a.ml_bytes = up256(all * sizeof(float2));
     return a;
@@ -563,9 +881,9 @@ Plan plan_attend(const squat_paged_store* s, int n_seqs, int64_t n_new, int q_pe
 // What the workspace query and the call itself ask of the sizes.
 int check_sizes(const squat_paged_store* s, int n_seqs, int64_t n_new, int q_per_kv, int pages_per_seq) {
     if (q_per_kv < 1 || q_per_kv > 16 || n_seqs < 0 || n_new < 0 || pages_per_seq < 0) return SQUAT_E_BADSHAPE;
-    if (n_new * q_per_kv > 0x3FFFFFFF) return SQUAT_E_BADSHAPE;
+    if (n_new * q_per_kv > 0x3FFFFFFF || n_seqs > 0x3FFFFFFF) return SQUAT_E_BADSHAPE;
     if (static_cast<int64_t>(pages_per_seq) * s->page_tokens > 0x3FFFFFFF) return SQUAT_E_BADSHAPE;
-    if ((n_new * q_per_kv / 16 + n_seqs) * s->n_kv_heads > 0x7FFFFFFF) return SQUAT_E_BADSHAPE;
+    if ((n_new * q_per_kv / 4 + n_seqs) * s->n_kv_heads > 0x7FFFFFFF) return SQUAT_E_BADSHAPE;
     return SQUAT_OK;
 }
 
@@ -575,8 +893,14 @@ void launch_rows(squat_dtype dt, dim3 grid, hipStream_t s, const AttendParams& p
     else hipLaunchKernelGGL((attend_kernel<BITS, NG, NQ, SQUAT_BF16>), grid, dim3(256), 0, s, p);
 }
 template <int BITS, int NG>
+void launch_few(squat_dtype dt, dim3 grid, hipStream_t s, const AttendParams& p) {
+    if (dt == SQUAT_F16) hipLaunchKernelGGL((attend_few_kernel<BITS, NG, SQUAT_F16>), grid, dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((attend_few_kernel<BITS, NG, SQUAT_BF16>), grid, dim3(256), 0, s, p);
+}
+template <int BITS, int NG>
 void launch_groups(int nq, squat_dtype dt, dim3 grid, hipStream_t s, const AttendParams& p) {
-    if (nq == 1) launch_rows<BITS, NG, 1>(dt, grid, s, p);
+    if (nq == 0) launch_few<BITS, NG>(dt, grid, s, p);
+    else if (nq == 1) launch_rows<BITS, NG, 1>(dt, grid, s, p);
     else launch_rows<BITS, NG, 2>(dt, grid, s, p);
 }
 template <int BITS>
@@ -651,13 +975,13 @@ extern "C" int squat_paged_attention(const squat_paged_store* store, const void*
     while ((1 << p.page_shift) < store->page_tokens) ++p.page_shift;
     p.scale = out_scale * kLog2e;
     p.splits = a.splits;
-    p.least = a.least;
+    p.span = a.span;
     p.n_tiles = static_cast<int>(a.tiles);
     p.part_o = static_cast<float*>(ws);
     p.part_ml = a.splits > 1 ? reinterpret_cast<float2*>(static_cast<unsigned char*>(ws) + a.o_bytes) : nullptr;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const unsigned gx = static_cast<unsigned>(a.tiles * store->n_kv_heads);
-    const dim3 grid(gx, static_cast<unsigned>(a.splits));
+    const dim3 grid(gx * static_cast<unsigned>(a.splits));
     switch (store->bits) {
         case 2: launch_bits<2>(store->group, a.nq, q_dt, grid, s, p); break;
         case 4: launch_bits<4>(store->group, a.nq, q_dt, grid, s, p); break;
@@ -665,7 +989,12 @@ extern "C" int squat_paged_attention(const squat_paged_store* store, const void*
     }
     rc = check_launch();
     if (rc || a.splits == 1) return rc;
-    if (a.nq == 1) launch_join<16>(q_dt, dim3(gx, 16), s, p);
-    else launch_join<32>(q_dt, dim3(gx, 32), s, p);
+    const dim3 rows(gx, static_cast<unsigned>(a.rows));
+    switch (a.rows) {
+        case 4: launch_join<4>(q_dt, rows, s, p); break;
+        case 8: launch_join<8>(q_dt, rows, s, p); break;
+        case 16: launch_join<16>(q_dt, rows, s, p); break;
+        default: launch_join<32>(q_dt, rows, s, p); break;
+    }
     return check_launch();
 }
