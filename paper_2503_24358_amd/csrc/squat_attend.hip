@@ -25,7 +25,11 @@ constexpr int kStep = 32;                                 // tokens per step of 
 constexpr int kWaves = 4;
 constexpr float kLift = 11.0f, kSlack = 4.0f;
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
-constexpr int kTarget = 8, kLeast = 8;                    // a launch's workgroups per compute unit, where there is work for them; a part's steps
+// A launch's workgroups per compute unit, where there is work for them: as many as it holds at once (three of a few rows, two of more), which
+// suits sequences that end together, and for the few rows of many sequences, whose lengths differ, more; and a part's steps at least.
+// us, 1 sequence of 131072 tokens, 8 query heads, 3 | 4 | 6 a compute unit 39.0 | 42.0 | 45.1; 64 ragged ones to 8192, 4 query heads, 6 | 8 | 12
+// 80.0 | 77.3 | 76.8; 16 of 6 tokens each to 4100, 8 bits, 2 | 4 | 8 36.4 | 40.1 | 44.4 (more rows, more sums to put together).
+constexpr int kTargetOne = 3, kTargetMany = 8, kTargetRows = 2, kLeast = 8;
 constexpr int kPitch = kD + 4;                            // floats per row of a wavefront's sums in LDS
 
 struct AttendParams {
@@ -149,6 +153,12 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t x, int b, const Places& c
     return (shifted(x, (BITS == 2 ? 6 : 4) - b) & c.mask) | c.bias;
 }
 
+// Where in a row of a step kept in LDS (see Stage) its 16-byte piece `piece` is.
+template <int BITS>
+__device__ __forceinline__ constexpr int turned(int row, int piece) {
+    return BITS == 2 ? piece : BITS == 4 ? piece ^ ((row >> 2) & 3) : piece ^ ((row >> 1) & 7);
+}
+
 // 32 channels of a key, the lane's quarter h, and 8 of them as an operand (step s), as bias + code.  `channel`: which of the 32 the
 // operand's element e is; the queries are held in that order.
 template <int BITS>
@@ -156,6 +166,7 @@ struct KeyWords;
 template <>
 struct KeyWords<2> {
     u32x2 w;
+    __device__ __forceinline__ void load_turned(const unsigned char* p, int m, int h) { w = *reinterpret_cast<const u32x2*>(p + 32 * m + 8 * h); }
     static __device__ __forceinline__ constexpr int channel(int s, int e) { return 16 * (s >> 1) + 4 * (s & 1) + (e >> 1) + 8 * (e & 1); }
     __device__ __forceinline__ void load(const unsigned char* p) { w = *reinterpret_cast<const u32x2*>(p); }
     __device__ __forceinline__ uint32_t pair(int s, int r, const Places& c) const { return code_pair<2>(w[s >> 1], 8 * (s & 1) + 2 * r, c); }
@@ -163,6 +174,9 @@ struct KeyWords<2> {
 template <>
 struct KeyWords<4> {
     u32x4 w;
+    __device__ __forceinline__ void load_turned(const unsigned char* p, int m, int h) {
+        w = *reinterpret_cast<const u32x4*>(p + 64 * m + 16 * turned<4>(m, h));
+    }
     static __device__ __forceinline__ constexpr int channel(int s, int e) { return 8 * s + (e >> 1) + 4 * (e & 1); }
     __device__ __forceinline__ void load(const unsigned char* p) { w = *reinterpret_cast<const u32x4*>(p); }
     __device__ __forceinline__ uint32_t pair(int s, int r, const Places& c) const { return code_pair<4>(w[s], 4 * r, c); }
@@ -170,6 +184,10 @@ struct KeyWords<4> {
 template <>
 struct KeyWords<8> {
     u32x4 w[2];
+    __device__ __forceinline__ void load_turned(const unsigned char* p, int m, int h) {
+        w[0] = *reinterpret_cast<const u32x4*>(p + 128 * m + 16 * turned<8>(m, 2 * h));
+        w[1] = *reinterpret_cast<const u32x4*>(p + 128 * m + 16 * turned<8>(m, 2 * h + 1));
+    }
     static __device__ __forceinline__ constexpr int channel(int s, int e) { return 8 * s + e; }
     __device__ __forceinline__ void load(const unsigned char* p) {
         w[0] = *reinterpret_cast<const u32x4*>(p);
@@ -184,6 +202,11 @@ struct KeyWords<8> {
 template <int BITS>
 struct ValueWord {
     typename std::conditional<BITS == 8, u32x2, typename std::conditional<BITS == 4, uint32_t, uint16_t>::type>::type w;
+    __device__ __forceinline__ void load_turned(const unsigned char* p, int row, int m) {
+        constexpr int ROW = kD * BITS / 8;
+        const int at = m * BITS;
+        w = *reinterpret_cast<const decltype(w)*>(p + row * ROW + 16 * turned<BITS>(row, at >> 4) + (at & 15));
+    }
 };
 
 // Channel j of two tokens, as bias + code.
@@ -292,8 +315,7 @@ __device__ __forceinline__ void load_query(const AttendParams& p, const unsigned
 
 // Row r of a tile from the wavefronts' sums (16 threads, 8 channels each; at: the row's place in `sums`): to the result or to the part's place.
 template <int R, int QDT, int N>
-__device__ __forceinline__ void finish_row(const AttendParams& p, const Tile& t, const Work& work, int r, const float (&sums)[kWaves][N][kPitch],
-                                           const float2 (&stats)[kWaves][R], int at) {
+__device__ __forceinline__ void finish_row(const AttendParams& p, const Tile& t, const Work& work, int r, const float (*sums)[N][kPitch], const float2 (*stats)[R], int at) {
     const int c0 = (static_cast<int>(threadIdx.x) & 15) * 8;
     const int row = t.row0 + r;
     if (row >= t.rows) return;
@@ -583,10 +605,74 @@ __global__ void __launch_bounds__(256) attend_kernel(const AttendParams p) {
         }
         __syncthreads();
         const int r = static_cast<int>(threadIdx.x) >> 4;
-        finish_row<R, QDT>(p, t, work, 16 * n + r, sums, stats, r);
+        finish_row<R, QDT, 16>(p, t, work, 16 * n + r, sums, stats, r);
         if (n + 1 < NQ) __syncthreads();
     }
 }
+
+// A wavefront's steps on their way: what a step reads is copied from memory to LDS, 16 bytes a lane, STAGES steps deep, without passing registers
+// (which leaves room for a fourth wavefront per SIMD) and with few, whole-line requests.  A step's place: the keys' codes of its two
+// halves, the values', then the scales and zero-points of the keys' and of the values' halves.  A row's 16-byte pieces are kept in an order that
+// goes round with the row, so that lanes reading one piece of many rows meet different banks.
+template <int BITS, int NG>
+struct Stage {
+    static constexpr int ROW = kD * BITS / 8, MROW = 4 * NG;
+    static constexpr int CODES = 32 * ROW, META = 32 * MROW, BYTES = 2 * CODES + 2 * META;
+    static constexpr int COPIES = 2 * (CODES / 1024) + 1;                    // instructions a step
+    static constexpr int STAGES = BITS == 2 ? 3 : 2;
+    uint32_t code_off[BITS == 8 ? 2 : 1];                 // of the lane's piece in a half step's codes
+    uint32_t meta_off;
+    int lane;
+    __device__ __forceinline__ explicit Stage(int l) : lane(l) {
+        if constexpr (BITS == 8) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int row = (l >> 3) + 8 * e;
+                code_off[e] = row * ROW + 16 * turned<BITS>(row, l & 7);
+            }
+        } else if constexpr (BITS == 4) {
+            code_off[0] = (l >> 2) * ROW + 16 * turned<BITS>(l >> 2, l & 3);
+        } else {
+            code_off[0] = 16 * (l & 31);
+        }
+        meta_off = 16 * (l % MROW);
+    }
+    typedef const __attribute__((address_space(1))) void* Global;
+    typedef __attribute__((address_space(3))) void* Local;
+    static __device__ __forceinline__ void copy(const unsigned char* from, unsigned char* to) {
+        __builtin_amdgcn_global_load_lds((Global)from, (Local)to, 16, 0, 0);
+    }
+    __device__ __forceinline__ void codes(const unsigned char* base, const Place& a, unsigned char* to) const {
+        const unsigned char *first = base + a.rows[0] * ROW, *second = base + a.rows[1] * ROW;
+        if constexpr (BITS == 2) {
+            copy((lane < 32 ? first : second) + code_off[0], to);
+        } else if constexpr (BITS == 4) {
+            copy(first + code_off[0], to);
+            copy(second + code_off[0], to + 1024);
+        } else {
+            copy(first + code_off[0], to);
+            copy(first + code_off[1], to + 1024);
+            copy(second + code_off[0], to + 2048);
+            copy(second + code_off[1], to + 3072);
+        }
+    }
+    __device__ __forceinline__ void fetch(const AttendParams& p, const Place& a, unsigned char* to) const {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                   // (what was read from this place has arrived)
+        codes(p.kc, a, to);
+        codes(p.vc, a, to + CODES);
+        if (lane < 4 * MROW) {
+            const unsigned char* k = p.km + (lane < MROW ? a.rows[0] : a.rows[1]) * MROW;
+            const unsigned char* v = p.vm + (lane < 3 * MROW ? a.rows[0] : a.rows[1]) * MROW;
+            copy((lane < 2 * MROW ? k : v) + meta_off, to + 2 * CODES);
+        }
+    }
+    // Waits until all but the newest N steps' copies have arrived.
+    template <int N>
+    static __device__ __forceinline__ void arrived() {
+        if constexpr (N * COPIES == 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N * COPIES) : "memory");
+    }
+};
 
 // A few rows, at most 16 / NG of a sequence and KV head (a decoded token's query heads): the matrix instructions' 16 columns hold every row
 // NG times, column n = (group g, row), so that scales need not enter the operands.
@@ -600,8 +686,13 @@ template <int BITS, int NG, int QDT>
 __global__ void __launch_bounds__(256) attend_few_kernel(const AttendParams p) {
     constexpr int R = 16 / NG;
     constexpr int ROW = kD * BITS / 8, MROW = 4 * NG;     // bytes of a token's codes, and of its scales and zero-points
-    __shared__ float sums[kWaves][R][kPitch];
-    __shared__ float2 stats[kWaves][R];
+    typedef Stage<BITS, NG> St;
+    constexpr int S = St::STAGES;
+    // The wavefronts' steps; in the end their sums, in the same place (40 KB for 4 bits in groups of 32: four workgroups a compute unit).
+    constexpr int STEPS = kWaves * S * St::BYTES, SUMS = kWaves * R * (kPitch * 4 + 8);
+    __shared__ __align__(16) unsigned char lds[STEPS > SUMS ? STEPS : SUMS];
+    float(*const sums)[R][kPitch] = reinterpret_cast<float(*)[R][kPitch]>(lds);
+    float2(*const stats)[R] = reinterpret_cast<float2(*)[R]>(lds + kWaves * R * kPitch * 4);
     const Work work(p);
     const int part = work.part, kvh = work.kvh;
     Tile t;
@@ -612,41 +703,27 @@ __global__ void __launch_bounds__(256) attend_few_kernel(const AttendParams p) {
     const int first = part * t.span, last = min(first + t.span, t.steps);
     const Walk walk(p, t, kvh);
 
-    // A step's loads.  Keys: the quarter h of lane m's token, and the column's group's scale and zero-point of the tokens 4 h + i.  Values: 8
-    // channels from 8 m on of the tokens 4 h + i, and the column's group's (which is those channels').
-    KeyWords<BITS> kw[2];
-    ValueWord<BITS> vw[2][4];
-    uint32_t km[2][4], vm[2][4];
-    const uint32_t k_at = m * ROW + h * (ROW / 4), v_at = 4 * h * ROW + m * BITS, m_at = 4 * h * MROW + 4 * g;
-    auto load_meta = [&](const unsigned char* from, uint32_t (&to)[4]) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) to[i] = *reinterpret_cast<const uint32_t*>(from + m_at + i * MROW);
-    };
-    auto load_keys = [&](const Place& a) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            kw[u].load(p.kc + a.rows[u] * ROW + k_at);
-            load_meta(p.km + a.rows[u] * MROW, km[u]);
+    // What a lane reads of a step.  Keys: the quarter h of row m, and the column's group's scale and zero-point of the rows 4 h + i.  Values: 8
+    // channels from 8 m on of the rows 4 h + i, and the column's group's (which is those channels').
+    const St st(lane);
+    unsigned char* const mine = lds + wave * (S * St::BYTES);
+    int step = first + wave, ahead_step = step;
+    Pages ahead{};
+    if (step < last) ahead = walk.pages(step);            // uniform
+    uint32_t missing = 0u;                                // places whose steps have a page that does not exist
+    const auto fetch = [&](int k) {                       // the step after the newest, if there is one, to place k
+        if (ahead_step < last) {
+            const Place at = walk.place(ahead_step, ahead);
+            missing = (missing & ~(1u << k)) | (at.limit[0] == 0 || at.limit[1] == 0 ? 1u << k : 0u);
+            ahead_step += kWaves;
+            ahead = walk.pages(ahead_step);               // (past the end: the last page's)
+            st.fetch(p, at, mine + k * St::BYTES);
+            return true;
         }
+        return false;
     };
-    auto load_values = [&](const Place& a) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const unsigned char* codes = p.vc + a.rows[u] * ROW;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) vw[u][i].w = *reinterpret_cast<const decltype(vw[u][i].w)*>(codes + v_at + i * ROW);
-            load_meta(p.vm + a.rows[u] * MROW, vm[u]);
-        }
-    };
-    int step = first + wave;
-    Place at;
-    Pages ahead;
-    if (step < last) {                                    // uniform
-        at = walk.place(step, walk.pages(step));
-        load_keys(at);
-        load_values(at);
-        ahead = walk.pages(step + kWaves);                // (past the end: the last page's)
-    }
+    for (int k = 0; k < S - 1; ++k) (void)fetch(k);
 
     // The query, brought to a largest element in [1/2, 1) by a power of two; of the column's group only.
     const int row = t.row0 + rr;
@@ -666,6 +743,12 @@ __global__ void __launch_bounds__(256) attend_few_kernel(const AttendParams p) {
 
     f32x4 o[8], weight = {0.0f, 0.0f, 0.0f, 0.0f};        // O^T: channels 8 (4 h + i) + j; the sum of p scale
     float top = -INFINITY, total = 0.0f, zeros = 0.0f;    // total: sum of p; zeros: sum of p zero (the lane's tokens)
+    // An fp16 result has three bits more than bf16's, and codes of one sign would carry the weights' rounding twice as far as values around zero do:
+    // there codes count from the middle of their range, whose part is a sum in the lane too (error against 64 bits, 1531 tokens, 4 bits,
+    // 4.2e-4 -> 2.8e-4; the result's own rounding is 2.1e-4).
+    constexpr bool CENTRED = QDT == SQUAT_F16;
+    constexpr float MIDDLE = CENTRED ? 0.5f * ((1 << BITS) - 1) : 0.0f;
+    float scales = 0.0f;
     int shift = -15;
     half8 ones;
 #pragma unroll
@@ -673,14 +756,21 @@ __global__ void __launch_bounds__(256) attend_few_kernel(const AttendParams p) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) o[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    while (step < last) {
+    int place = 0;
+    for (; step < last; step += kWaves) {
         const int t0 = step * kStep;
-        const int limit0 = at.limit[0], limit1 = at.limit[1];
-        step += kWaves;
-        const bool more = step < last;
-        if (more) {
-            at = walk.place(step, ahead);
-            ahead = walk.pages(step + kWaves);
+        // (the copies of the newest S - 1 steps, where there are as many)
+        if (fetch(place == 0 ? S - 1 : place - 1)) St::template arrived<S - 1>();
+        else St::template arrived<0>();
+        const unsigned char* const now_at = mine + place * St::BYTES;
+        KeyWords<BITS> kw[2];
+        uint32_t km[2][4];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            kw[u].load_turned(now_at + u * (St::CODES / 2), m, h);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                km[u][i] = *reinterpret_cast<const uint32_t*>(now_at + 2 * St::CODES + u * (St::META / 2) + (4 * h + i) * MROW + 4 * g);
         }
 
         // logits: the tokens t0 + 16 u + 4 h + i
@@ -705,17 +795,26 @@ __global__ void __launch_bounds__(256) attend_few_kernel(const AttendParams p) {
                 x[u][i] = y;
             }
         }
-        if (more) load_keys(at);                          // (in flight behind the values', which come back first)
+        ValueWord<BITS> vw[2][4];
+        uint32_t vm[2][4];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                vw[u][i].load_turned(now_at + St::CODES + u * (St::CODES / 2), 4 * h + i, m);
+                vm[u][i] = *reinterpret_cast<const uint32_t*>(now_at + 2 * St::CODES + St::META + u * (St::META / 2) + (4 * h + i) * MROW + 4 * g);
+            }
 
         // the last tokens, the ones that not every row sees, and pages that do not exist
-        const bool edge = t0 + kStep > least_seen + 1 || t0 + 16 > limit0 || t0 + kStep > limit1;       // uniform
+        const bool edge = t0 + kStep > least_seen + 1 || t0 + kStep > t.end || (missing >> place & 1u);          // uniform
         if (edge) {
+            const Place here = walk.place(step, walk.pages(step));
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int token = t0 + 16 * u + 4 * h + i;
-                    if (token < (u ? limit1 : limit0) && token <= seen) continue;
+                    if (token < here.limit[u] && token <= seen) continue;
                     x[u][i] = -INFINITY;
                     vm[u][i] = 0u;                        // whatever the page holds there: NaN and infinity are in the scales alone
                 }
@@ -741,6 +840,7 @@ __global__ void __launch_bounds__(256) attend_few_kernel(const AttendParams p) {
             shift = up;
             total *= by;
             zeros *= by;
+            if constexpr (CENTRED) scales *= by;
             weight *= by;
 #pragma unroll
             for (int j = 0; j < 8; ++j) o[j] *= by;
@@ -754,6 +854,7 @@ __global__ void __launch_bounds__(256) attend_few_kernel(const AttendParams p) {
             total += w;
             zeros = fmaf(half_hi(sz), w, zeros);
             pf[e] = static_cast<_Float16>(half_lo(sz) * w);
+            if constexpr (CENTRED) scales = fmaf(half_lo(sz), w, scales);
         }
         weight = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pf, weight, 0, 0, 0);
 
@@ -765,7 +866,7 @@ __global__ void __launch_bounds__(256) attend_few_kernel(const AttendParams p) {
             for (int e = 0; e < 4; ++e) c[e] = value_pair<BITS>(vw[e >> 1][2 * (e & 1)], vw[e >> 1][2 * (e & 1) + 1], j, places_);
             o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, c), pf, o[j], 0, 0, 0);
         }
-        if (more) load_values(at);
+        place = place + 1 == S ? 0 : place + 1;
     }
 
     // The four wavefronts' sums.  A lane has its column's group where its channels, 32 h to 32 h + 31, are of that group.
@@ -773,7 +874,13 @@ __global__ void __launch_bounds__(256) attend_few_kernel(const AttendParams p) {
     total += __shfl_xor(total, 32, 64);
     zeros += __shfl_xor(zeros, 16, 64);
     zeros += __shfl_xor(zeros, 32, 64);
-    const float back = ldexpf(1.0f, shift), add = fmaf(-Bias<BITS>::value, weight[0], zeros);
+    if constexpr (CENTRED) {
+        scales += __shfl_xor(scales, 16, 64);
+        scales += __shfl_xor(scales, 32, 64);
+        zeros = fmaf(MIDDLE, scales, zeros);
+    }
+    const float back = ldexpf(1.0f, shift), add = fmaf(-(Bias<BITS>::value + MIDDLE), weight[0], zeros);
+    __syncthreads();                                      // (nobody reads steps any more)
     if (h == 0 && g == 0) stats[wave][rr] = float2{top > -INFINITY ? top * scale : -INFINITY, total * back};
     if ((h * NG) >> 2 == g) {
 #pragma unroll
@@ -785,60 +892,87 @@ __global__ void __launch_bounds__(256) attend_few_kernel(const AttendParams p) {
     }
     __syncthreads();
     const int r = static_cast<int>(threadIdx.x) >> 4;
-    if (r < R) finish_row<R, QDT>(p, t, work, r, sums, stats, r);
+    if (r < R) finish_row<R, QDT, R>(p, t, work, r, sums, stats, r);
 }
 
-// The parts of a row put together: one workgroup a row, a wavefront every fourth part, two channels a lane.
-template <int R, int QDT>
+// The parts of a row put together: half a wavefront a part (16 bytes a lane), WAVES wavefronts a row, so that for WAVES = 4 a row's first 128
+// parts are asked for at once; what the parts weigh is asked for with them.
+template <int R, int WAVES, int QDT>
 __global__ void __launch_bounds__(256) attend_join_kernel(const AttendParams p) {
-    __shared__ float2 sums[kWaves][64];
-    __shared__ float totals[kWaves];
-    const int bx = static_cast<int>(blockIdx.x), w_tile = bx / p.n_kv, kvh = bx - w_tile * p.n_kv;
-    Tile t;
-    if (!find_tile<R>(p, w_tile, t)) return;
-    const int row = t.row0 + static_cast<int>(blockIdx.y);
-    if (row >= t.rows) return;
-    const int lane = static_cast<int>(threadIdx.x) & 63;
+    constexpr int ROWS = kWaves / WAVES, AT_ONCE = WAVES == 1 ? 4 : 16;
+    __shared__ f32x4 sums[WAVES == 1 ? 1 : kWaves][32];
+    __shared__ float2 stats[WAVES == 1 ? 1 : kWaves];
+    const int lane = static_cast<int>(threadIdx.x) & 63, half = lane >> 5, c = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
-    const int64_t at = static_cast<int64_t>(bx) * R + blockIdx.y, stride = static_cast<int64_t>(p.n_tiles) * p.n_kv * R;
-    float all = -INFINITY;
-    for (int s = lane; s < t.parts; s += 64) all = fmaxf(all, p.part_ml[at + s * stride].x);
+    constexpr int BLOCKS = R / ROWS;                      // per tile and head
+    const uint32_t b = blockIdx.x / BLOCKS, w_tile = b / static_cast<uint32_t>(p.n_kv);
+    const int kvh = static_cast<int>(b - w_tile * p.n_kv);
+    const int r = static_cast<int>(blockIdx.x % BLOCKS) * ROWS + (WAVES == 1 ? wave : 0);
+    Tile t;
+    if (!find_tile<R>(p, static_cast<int>(w_tile), t)) return;
+    const int row = t.row0 + r;
+    if (row >= t.rows) return;                            // (WAVES = 4: the same for the workgroup)
+    const int64_t at = (static_cast<int64_t>(w_tile) * p.n_kv + kvh) * R + r, stride = static_cast<int64_t>(p.n_tiles) * p.n_kv * R;
+    float top = -INFINITY, sum = 0.0f;
+    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s0 = (WAVES == 1 ? 0 : 2 * wave) + half; s0 - half < t.parts; s0 += 2 * WAVES * AT_ONCE) {        // uniform
+        float2 ml[AT_ONCE];
+        f32x4 v[AT_ONCE];
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor(all, o, 64));
-    float2 acc{0.0f, 0.0f};
-    float sum = 0.0f;
-#pragma unroll 4
-    for (int s = wave; s < t.parts; s += kWaves) {
-        const float2 ml = p.part_ml[at + s * stride];
-        const float2 v = *reinterpret_cast<const float2*>(p.part_o + (at + s * stride) * kD + 2 * lane);
-        const float by = ml.x > -INFINITY ? __builtin_amdgcn_exp2f(ml.x - all) : 1.0f;
-        sum += by * ml.y;
-        acc.x = fmaf(by, v.x, acc.x);
-        acc.y = fmaf(by, v.y, acc.y);
-    }
-    sums[wave][lane] = acc;
-    if (lane == 0) totals[wave] = sum;
-    __syncthreads();
-    if (wave != 0) return;
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int s = min(s0 + 2 * WAVES * k, t.parts - 1);               // (beyond the last: read again, and not counted)
+            ml[k] = p.part_ml[at + s * stride];
+            v[k] = *reinterpret_cast<const f32x4*>(p.part_o + (at + s * stride) * kD + 4 * c);
+        }
+        float now = top;
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) {
-        acc.x += sums[w][lane].x;
-        acc.y += sums[w][lane].y;
-        sum += totals[w];
+        for (int k = 0; k < AT_ONCE; ++k) {
+            if (s0 + 2 * WAVES * k >= t.parts) ml[k] = float2{-INFINITY, 0.0f}, v[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            now = fmaxf(now, ml[k].x);
+        }
+        const float keep = top > -INFINITY ? __builtin_amdgcn_exp2f(top - now) : 1.0f;
+        top = now;
+        sum *= keep;
+        acc *= keep;
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const float by = ml[k].x > -INFINITY ? __builtin_amdgcn_exp2f(ml[k].x - top) : 1.0f;
+            sum = fmaf(by, ml[k].y, sum);
+            acc += v[k] * by;
+        }
     }
+    const auto add = [&](float top2, float sum2, const f32x4& acc2) {
+        const float now = fmaxf(top, top2);
+        const float one = top > -INFINITY ? __builtin_amdgcn_exp2f(top - now) : 1.0f, two = top2 > -INFINITY ? __builtin_amdgcn_exp2f(top2 - now) : 1.0f;
+        top = now;
+        sum = sum * one + sum2 * two;
+        acc = acc * one + acc2 * two;
+    };
+    {
+        const f32x4 other = {__shfl_xor(acc[0], 32, 64), __shfl_xor(acc[1], 32, 64), __shfl_xor(acc[2], 32, 64), __shfl_xor(acc[3], 32, 64)};
+        add(__shfl_xor(top, 32, 64), __shfl_xor(sum, 32, 64), other);
+    }
+    if constexpr (WAVES > 1) {
+        if (half == 0) sums[wave][c] = acc;
+        if (lane == 0) stats[wave] = float2{top, sum};
+        __syncthreads();
+        if (wave != 0) return;
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) add(stats[w].x, stats[w].y, sums[w][c]);
+    }
+    if (half != 0) return;
     const int i = row / p.qpk, hq = kvh * p.qpk + (row - i * p.qpk);
     const float by = sum == 0.0f ? 1.0f : 1.0f / sum;
-    unsigned char* to = p.out + ((t.start + i) * p.ost + hq * p.osh + 2 * lane) * 2;
-    uint32_t both;
+    unsigned char* to = p.out + ((t.start + i) * p.ost + hq * p.osh + 4 * c) * 2;
     if constexpr (QDT == SQUAT_BF16) {
-        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-        both = __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(acc.x * by), static_cast<__bf16>(acc.y * by)});
+        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+        *reinterpret_cast<bf16x4*>(to) = bf16x4{static_cast<__bf16>(acc[0] * by), static_cast<__bf16>(acc[1] * by), static_cast<__bf16>(acc[2] * by), static_cast<__bf16>(acc[3] * by)};
     } else {
-        both = __builtin_bit_cast(uint32_t, half2v{static_cast<_Float16>(acc.x * by), static_cast<_Float16>(acc.y * by)});
+        typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+        *reinterpret_cast<half4*>(to) = half4{static_cast<_Float16>(acc[0] * by), static_cast<_Float16>(acc[1] * by), static_cast<_Float16>(acc[2] * by), static_cast<_Float16>(acc[3] * by)};
     }
-    *reinterpret_cast<uint32_t*>(to) = both;
-    if (p.lse && lane == 0)
-        p.lse[static_cast<int64_t>(t.start + i) * p.n_kv * p.qpk + hq] = sum == 0.0f ? -INFINITY : kLn2 * ((all - kLift) + __builtin_amdgcn_logf(sum));
+    if (p.lse && c == 0)
+        p.lse[static_cast<int64_t>(t.start + i) * p.n_kv * p.qpk + hq] = sum == 0.0f ? -INFINITY : kLn2 * ((top - kLift) + __builtin_amdgcn_logf(sum));
 }
 
 struct Plan {
@@ -862,13 +996,14 @@ Plan plan_attend(const squat_paged_store* s, int n_seqs, int64_t n_new, int q_pe
     // tiles with work: what the hints allow
     int64_t busy = n_seqs * ((max_new * q_per_kv + a.rows - 1) / a.rows);
     busy = (busy < a.tiles ? busy : a.tiles) * s->n_kv_heads;
-    const int64_t steps = (max_kv + kStep - 1) / kStep, wanted = (kTarget * device_cu_count() + busy - 1) / busy;
+    const int64_t steps = (max_kv + kStep - 1) / kStep, wanted = ((a.nq > 0 ? kTargetRows : n_seqs < 4 ? kTargetOne : kTargetMany) * device_cu_count() + busy - 1) / busy;
     int64_t span = (steps + wanted - 1) / wanted;
     span = span < kLeast ? kLeast : span;
     int64_t n = (steps + span - 1) / span;
     n = n > 256 ? 256 : n;
-    const int64_t room_for = 0x7FFFFFFF / (a.tiles * s->n_kv_heads);        // (one dimension of workgroups)
-    n = n > room_for ? room_for : n;
+    // (one dimension of workgroups, here and where the parts are put together)
+    const int64_t room_for = 0x7FFFFFFF / (a.tiles * s->n_kv_heads);
+    n = a.rows > room_for ? 1 : n > room_for ? room_for : n;
     a.splits = n < 1 ? 1 : static_cast<int>(n);
     a.span = static_cast<int>((steps + a.splits - 1) / a.splits);
     a.span = a.span < 1 ? 1 : a.span;
@@ -911,10 +1046,18 @@ void launch_bits(int group, int nq, squat_dtype dt, dim3 grid, hipStream_t s, co
         default: launch_groups<BITS, 1>(nq, dt, grid, s, p); break;
     }
 }
+// A wavefront a row where there are few parts, four where there are many.
 template <int R>
-void launch_join(squat_dtype dt, dim3 grid, hipStream_t s, const AttendParams& p) {
-    if (dt == SQUAT_F16) hipLaunchKernelGGL((attend_join_kernel<R, SQUAT_F16>), grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((attend_join_kernel<R, SQUAT_BF16>), grid, dim3(256), 0, s, p);
+void launch_join(squat_dtype dt, unsigned tiles, hipStream_t s, const AttendParams& p) {
+    if (p.splits <= 16) {
+        const dim3 grid(tiles * (R / kWaves));
+        if (dt == SQUAT_F16) hipLaunchKernelGGL((attend_join_kernel<R, 1, SQUAT_F16>), grid, dim3(256), 0, s, p);
+        else hipLaunchKernelGGL((attend_join_kernel<R, 1, SQUAT_BF16>), grid, dim3(256), 0, s, p);
+    } else {
+        const dim3 grid(tiles * R);
+        if (dt == SQUAT_F16) hipLaunchKernelGGL((attend_join_kernel<R, 4, SQUAT_F16>), grid, dim3(256), 0, s, p);
+        else hipLaunchKernelGGL((attend_join_kernel<R, 4, SQUAT_BF16>), grid, dim3(256), 0, s, p);
+    }
 }
 
 }  // namespace
@@ -989,12 +1132,11 @@ extern "C" int squat_paged_attention(const squat_paged_store* store, const void*
     }
     rc = check_launch();
     if (rc || a.splits == 1) return rc;
-    const dim3 rows(gx, static_cast<unsigned>(a.rows));
     switch (a.rows) {
-        case 4: launch_join<4>(q_dt, rows, s, p); break;
-        case 8: launch_join<8>(q_dt, rows, s, p); break;
-        case 16: launch_join<16>(q_dt, rows, s, p); break;
-        default: launch_join<32>(q_dt, rows, s, p); break;
+        case 4: launch_join<4>(q_dt, gx, s, p); break;
+        case 8: launch_join<8>(q_dt, gx, s, p); break;
+        case 16: launch_join<16>(q_dt, gx, s, p); break;
+        default: launch_join<32>(q_dt, gx, s, p); break;
     }
     return check_launch();
 }

@@ -1,9 +1,10 @@
 // squat_paged_write / squat_paged_read: tokens into and out of a store of pages (Section 2's quantizer, per token and group of
 // channels; keys with an update matrix go through the kernel of squat_quantize_keys and are then dealt to their slots).
 //
-// Bound: HBM (a token-head in bf16 moves 512 bytes of keys and values and, 4 bits, groups of 32, 160 of store), for a few
-// tokens the launch.  Eight lanes hold the 128 channels of a token-head, 16 each: a group's statistics are two or three lane
-// exchanges, and a wavefront takes eight consecutive tokens of one head, whose rows lie next to each other in a page.
+// Bound: HBM (a token-head in bf16 moves 512 bytes of keys and values and, 4 bits, groups of 32, 160 of store), the writing kernel also the
+// vector instructions (about 9 a value), for a few tokens the launch.  Sixteen lanes hold the 128 channels of a token-head, 8 each, so that
+// every load and store instruction covers whole lines of 16-bit tokens, and a group's statistics are two to four exchanges within
+// sixteen lanes; a workgroup takes sixteen consecutive tokens of one head, whose rows lie next to each other in a page.
 #include "squat_paged.h"
 #include "squat_residual.h"
 
@@ -11,7 +12,8 @@ using namespace squat;
 
 namespace {
 
-constexpr int kTokens = 32;                               // tokens of one head per workgroup of 256 threads
+constexpr int kTokens = 16;                               // tokens of one head per workgroup of 256 threads
+constexpr int kLane = 8;                                  // channels a lane
 
 struct PagedRows {
     uint32_t* codes[2];                                   // keys, values
@@ -21,16 +23,37 @@ struct PagedRows {
     int64_t n;
     int n_heads;
     int page_shift;
-    int group;
+    int group_shift;                                      // log2 of the channels a group
     int first;                                            // blockIdx.z 0 is this one
 };
 
-// The row of (slot, head) in an array of pages, or -1.
-__device__ __forceinline__ int64_t store_row(const PagedRows& p, int64_t t, int h) {
-    const int64_t slot = p.slots[t];
-    if (slot < 0 || slot >= p.n_slots) return -1;
-    const int64_t page = slot >> p.page_shift;
-    return (((page * p.n_heads + h) << p.page_shift)) + (slot & ((int64_t(1) << p.page_shift) - 1));
+// A lane's token: the row of its slot in an array of pages (or none), and where its channels are in a tensor of tokens.  (What the workgroup has in
+// common is worked out in scalars; pages are below 2^31.)
+struct Mine {
+    int h, which, part, in_block;
+    bool live;                                            // a token of the call
+    uint64_t row;
+    bool stored;                                          // its slot is in the store
+    __device__ __forceinline__ explicit Mine(const PagedRows& p) {
+        h = static_cast<int>(blockIdx.y);
+        which = static_cast<int>(blockIdx.z) + p.first;
+        part = static_cast<int>(threadIdx.x) & 15;
+        in_block = static_cast<int>(threadIdx.x) >> 4;
+        const int64_t first = static_cast<int64_t>(blockIdx.x) * kTokens;
+        live = in_block < p.n - first;
+        const uint64_t slot = static_cast<uint64_t>(p.slots[first + (live ? in_block : 0)]);
+        stored = live && slot < static_cast<uint64_t>(p.n_slots);
+        const uint32_t page = static_cast<uint32_t>(slot >> p.page_shift), within = static_cast<uint32_t>(slot) & ((1u << p.page_shift) - 1u);
+        row = ((static_cast<uint64_t>(page) * static_cast<uint32_t>(p.n_heads) + static_cast<uint32_t>(h)) << p.page_shift) | within;
+    }
+    __device__ __forceinline__ int64_t at(int64_t st, int64_t sh, int bytes) const {
+        return static_cast<int64_t>(blockIdx.x) * kTokens * st + h * sh + (static_cast<int64_t>(in_block) * st + part * bytes);
+    }
+};
+
+// Where the scale and zero-point of a lane's channels are.
+__device__ __forceinline__ uint64_t meta_at(const PagedRows& p, uint64_t row, int part) {
+    return (row << (7 - p.group_shift)) + (part >> (p.group_shift - 3));
 }
 
 struct WriteParams {
@@ -39,72 +62,124 @@ struct WriteParams {
     int64_t st, sh;                                       // strides in BYTES
 };
 
-// A group's codes are decided as in 64 bits: u = (x - zero) / scale in fp32 is off by less than 2^-21 u, so only a value that lies
-// closer than that to a rounding border (k + 1/2) needs the quotient itself; then the lane's channels are done again in fp64.
+__device__ __forceinline__ float raw_min3(float a, float b, float c) {
+    float r;
+    asm("v_min3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+__device__ __forceinline__ float raw_max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
+// f over aligned runs of `lanes` (4, 8 or 16) lanes: neighbours, pairs, then halves turned round.
+template <int CTRL>
+__device__ __forceinline__ float moved(float x) {
+    return as_f32(static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(as_u32(x)), CTRL, 0xF, 0xF, true)));
+}
+template <typename F>
+__device__ __forceinline__ float over_lanes(float x, int lanes, F f) {
+    x = f(x, moved<0xB1>(x));
+    x = f(x, moved<0x4E>(x));
+    if (lanes >= 8) x = f(x, moved<0x141>(x));            // uniform
+    if (lanes >= 16) x = f(x, moved<0x140>(x));
+    return x;
+}
+
+// A lane's 8 codes, BITS / 2 halves of a word.
+template <int BITS>
+struct Codes {
+    uint32_t half[BITS / 2];
+    __device__ __forceinline__ void store(uint32_t* row, int part) const {
+        if constexpr (BITS == 2) reinterpret_cast<uint16_t*>(row)[part] = static_cast<uint16_t>(half[0]);
+        else if constexpr (BITS == 4) row[part] = half[0] | (half[1] << 16);
+        else *reinterpret_cast<u32x2*>(row + 2 * part) = u32x2{half[0] | (half[1] << 16), half[2] | (half[3] << 16)};
+    }
+    __device__ __forceinline__ void load(const uint32_t* row, int part) {
+        if constexpr (BITS == 2) {
+            half[0] = reinterpret_cast<const uint16_t*>(row)[part];
+        } else if constexpr (BITS == 4) {
+            const uint32_t w = row[part];
+            half[0] = w & 0xFFFFu;
+            half[1] = w >> 16;
+        } else {
+            const u32x2 w = *reinterpret_cast<const u32x2*>(row + 2 * part);
+            half[0] = w[0] & 0xFFFFu;
+            half[1] = w[0] >> 16;
+            half[2] = w[1] & 0xFFFFu;
+            half[3] = w[1] >> 16;
+        }
+    }
+};
+
+// A group's codes are decided as in 64 bits.  The quotient in fp32, x / scale - zero / scale with |zero| / scale at most FAR, is off by less than
+// 2^-13 for 8 bits and 2^-17 for fewer, and the code of its nearest whole number is in its range: only where it lies closer than that to a
+// rounding border (k + 1/2), or the offset is larger or the scale subnormal, are the lane's channels done again, in fp64.
 template <int BITS, int DT>
 __global__ void __launch_bounds__(256) paged_write_kernel(const WriteParams p) {
     constexpr int ES = DT == SQUAT_F32 ? 4 : 2;
-    constexpr int NW = BITS / 2;                          // words of a lane's 16 codes
+    constexpr int PER = 16 / BITS;                        // codes a half word
     constexpr float TOP = static_cast<float>((1 << BITS) - 1);
-    constexpr float NEAR = BITS == 8 ? 0.4998f : 0.49999f;
-    const int part = static_cast<int>(threadIdx.x) & 7;
-    const int64_t t = static_cast<int64_t>(blockIdx.x) * kTokens + (threadIdx.x >> 3);
-    if (t >= p.rows.n) return;                            // the same for the eight lanes
-    const int h = static_cast<int>(blockIdx.y);
-    const int which = static_cast<int>(blockIdx.z) + p.rows.first;
-    const unsigned char* src = p.x[which] + t * p.st + h * p.sh + part * (16 * ES);
-    float x[16];
-    load8<DT>(src, x);
-    load8<DT>(src + 8 * ES, x + 8);
-    const int64_t row = store_row(p.rows, t, h);
-    float mn = x[0], mx = x[0], bad = 0.0f;               // bad: NaN if a channel is infinite or NaN
+    constexpr float NEAR = BITS == 8 ? 0.4998f : 0.49999f, FAR = BITS == 8 ? 256.0f : kQuantFastOffset;
+    const Mine mine(p.rows);
+    if (!mine.live) return;                               // the same for the sixteen lanes
+    const int part = mine.part, which = mine.which;
+    float x[kLane];
+    load8<DT>(p.x[which] + mine.at(p.st, p.sh, kLane * ES), x);
+    const float mn01 = raw_min(x[0], x[1]), mx01 = raw_max(x[0], x[1]);
+    float mn = raw_min3(raw_min3(mn01, x[2], x[3]), raw_min3(x[4], x[5], x[6]), x[7]);
+    float mx = raw_max3(raw_max3(mx01, x[2], x[3]), raw_max3(x[4], x[5], x[6]), x[7]);
+    float bad = 0.0f;                                     // NaN if a channel is infinite or NaN
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        mn = fminf(mn, x[e]);
-        mx = fmaxf(mx, x[e]);
-        bad = fmaf(x[e], 0.0f, bad);
-    }
-    for (int o = 1; o < p.rows.group / 16; o <<= 1) {     // uniform
-        mn = fminf(mn, __shfl_xor(mn, o, 64));
-        mx = fmaxf(mx, __shfl_xor(mx, o, 64));
-        bad += __shfl_xor(bad, o, 64);
-    }
-    if (row < 0) return;
-    const float step = static_cast<float>((static_cast<double>(mx) - static_cast<double>(mn)) / static_cast<double>(TOP));
+    for (int e = 0; e < kLane; ++e) bad = fmaf(x[e], 0.0f, bad);
+    const int lanes = 1 << (p.rows.group_shift - 3);
+    mn = over_lanes(mn, lanes, raw_min);
+    mx = over_lanes(mx, lanes, raw_max);
+    bad = over_lanes(bad, lanes, [](float a, float b) { return a + b; });
+    if (!mine.stored) return;
+    const uint64_t row = mine.row;
+    // (max - min) / (2^b - 1), rounded to fp32: the difference as two numbers, the quotient from its remainder
+    const float range = mx - mn, rest = (mx - (range + mn)) + ((range + mn) - range - mn);
+    constexpr float RT = 1.0f / TOP;
+    const float q0 = range * RT, step = fmaf(fmaf(-q0, TOP, range) + rest, RT, q0);
     uint16_t sbits, zbits;
     const float s = round_f16(step + bad, sbits), z = round_f16(mn + bad, zbits);
     const bool live = s > 0.0f;
-    const float inv = 1.0f / (live ? s : 1.0f);
-    uint32_t words[NW];
+    const float sp = live ? s : 1.0f;
+    float inv = __builtin_amdgcn_rcpf(sp);
+    inv = fmaf(fmaf(-sp, inv, 1.0f), inv, inv);
+    const float offset = -z * inv;
+    float away = s >= 6.2e-5f && fabsf(offset) <= FAR ? 0.0f : 1.0f;          // from the nearest whole number, at most
+    Codes<BITS> c;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) words[w] = 0u;
-    bool near = false;
+    for (int q = 0; q < BITS / 2; ++q) {
+        float all = 0.0f;                                 // below 2^16: exact
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        const float u = (x[e] - z) * inv, r = rintf(u);
-        near |= fabsf(u - r) > NEAR;
-        const uint32_t c = live ? static_cast<uint32_t>(fminf(fmaxf(r, 0.0f), TOP)) : 0u;
-        words[e * BITS / 32] |= c << (e * BITS % 32);
+        for (int e = PER - 1; e >= 0; --e) {
+            const float u = fmaf(x[PER * q + e], inv, offset), r = __builtin_rintf(u);
+            away = raw_max(away, fabsf(u - r));
+            all = fmaf(all, static_cast<float>(1 << BITS), r);
+        }
+        c.half[q] = live ? static_cast<uint32_t>(all) : 0u;
     }
-    if (near && live) {
+    if (__ballot(live && away > NEAR)) {                  // (a branch for the wavefront: half of the instructions are here)
 #pragma unroll
-        for (int w = 0; w < NW; ++w) words[w] = 0u;
+        for (int q = 0; q < BITS / 2; ++q) {
+            uint32_t half = 0u;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const double r = rint((static_cast<double>(x[e]) - static_cast<double>(z)) / static_cast<double>(s));
-            const uint32_t c = static_cast<uint32_t>(fmin(fmax(r, 0.0), static_cast<double>(TOP)));
-            words[e * BITS / 32] |= c << (e * BITS % 32);
+            for (int e = 0; e < PER; ++e) {
+                const double r = rint((static_cast<double>(x[PER * q + e]) - static_cast<double>(z)) / static_cast<double>(sp));
+                half |= static_cast<uint32_t>(fmin(fmax(r, 0.0), static_cast<double>(TOP))) << (BITS * e);
+            }
+            if (live && away > NEAR) c.half[q] = half;
         }
     }
-    uint32_t* out = p.rows.codes[which] + row * (kD * BITS / 32) + part * NW;
-    if constexpr (NW == 1) out[0] = words[0];
-    else if constexpr (NW == 2) *reinterpret_cast<u32x2*>(out) = u32x2{words[0], words[1]};
-    else *reinterpret_cast<u32x4*>(out) = u32x4{words[0], words[1], words[2], words[3]};
-    if ((part * 16) % p.rows.group == 0)
-        p.rows.meta[which][row * (kD / p.rows.group) + part * 16 / p.rows.group] = sbits | (static_cast<uint32_t>(zbits) << 16);
+    c.store(p.rows.codes[which] + row * (kD * BITS / 32), part);
+    if ((part & (lanes - 1)) == 0) p.rows.meta[which][meta_at(p.rows, row, part)] = sbits | (static_cast<uint32_t>(zbits) << 16);
 }
 
-// Rows that squat_quantize_keys' kernel wrote densely, [heads, n, ...], to their slots: eight lanes a row.
+// Rows that squat_quantize_keys' kernel wrote densely, [heads, n, ...], to their slots.
 struct DealParams {
     PagedRows rows;
     const uint32_t* codes;
@@ -113,18 +188,15 @@ struct DealParams {
 
 template <int BITS>
 __global__ void __launch_bounds__(256) paged_deal_kernel(const DealParams p) {
-    constexpr int NW = BITS / 2;
-    const int part = static_cast<int>(threadIdx.x) & 7;
-    const int64_t t = static_cast<int64_t>(blockIdx.x) * kTokens + (threadIdx.x >> 3);
-    if (t >= p.rows.n) return;
-    const int h = static_cast<int>(blockIdx.y);
-    const int64_t row = store_row(p.rows, t, h);
-    if (row < 0) return;
-    const int64_t from = h * p.rows.n + t;
-#pragma unroll
-    for (int w = 0; w < NW; ++w)
-        p.rows.codes[0][row * (kD * BITS / 32) + part * NW + w] = p.codes[from * (kD * BITS / 32) + part * NW + w];
-    const int ng = kD / p.rows.group;
+    const Mine mine(p.rows);
+    if (!mine.stored) return;
+    const int part = mine.part;
+    const uint64_t row = mine.row;
+    const int64_t from = mine.h * p.rows.n + static_cast<int64_t>(blockIdx.x) * kTokens + mine.in_block;
+    Codes<BITS> c;
+    c.load(p.codes + from * (kD * BITS / 32), part);
+    c.store(p.rows.codes[0] + row * (kD * BITS / 32), part);
+    const int ng = kD >> p.rows.group_shift;
     if (part < ng) p.rows.meta[0][row * ng + part] = p.scale[from * ng + part] | (static_cast<uint32_t>(p.zero[from * ng + part]) << 16);
 }
 
@@ -134,67 +206,50 @@ struct ReadParams {
     int64_t st, sh;                                       // strides in BYTES
 };
 
-// 16 values of one lane, rounded once
+__device__ __forceinline__ void put16(unsigned char* to, const u32x4& v) { __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(to)); }
+
+// A lane's 8 values, rounded once, past the caches: a store instruction writes whole lines, which nobody here reads again.
 template <int DT>
-__device__ __forceinline__ void store16(unsigned char* to, const float (&x)[16]) {
+__device__ __forceinline__ void store8(unsigned char* to, const float (&x)[kLane]) {
     if constexpr (DT == SQUAT_F32) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4*>(to + 16 * i) = f32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+        for (int i = 0; i < 2; ++i)
+            *reinterpret_cast<f32x4*>(to + 16 * i) = f32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
     } else if constexpr (DT == SQUAT_F16) {
+        half8 v;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            half8 v;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = static_cast<_Float16>(x[8 * i + e]);
-            *reinterpret_cast<half8*>(to + 16 * i) = v;
-        }
+        for (int e = 0; e < 8; ++e) v[e] = static_cast<_Float16>(x[e]);
+        put16(to, __builtin_bit_cast(u32x4, v));
     } else {
+        bf16x8 v;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            bf16x8 v;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = static_cast<__bf16>(x[8 * i + e]);
-            *reinterpret_cast<bf16x8*>(to + 16 * i) = v;
-        }
+        for (int e = 0; e < 8; ++e) v[e] = static_cast<__bf16>(x[e]);
+        put16(to, __builtin_bit_cast(u32x4, v));
     }
 }
 
 template <int BITS, int DT>
 __global__ void __launch_bounds__(256) paged_read_kernel(const ReadParams p) {
     constexpr int ES = DT == SQUAT_F32 ? 4 : 2;
-    constexpr int NW = BITS / 2;
-    const int part = static_cast<int>(threadIdx.x) & 7;
-    const int64_t t = static_cast<int64_t>(blockIdx.x) * kTokens + (threadIdx.x >> 3);
-    if (t >= p.rows.n) return;
-    const int h = static_cast<int>(blockIdx.y);
-    const int which = static_cast<int>(blockIdx.z) + p.rows.first;
-    const int64_t row = store_row(p.rows, t, h);
-    float x[16];
-    if (row < 0) {
+    constexpr int PER = 16 / BITS;
+    const Mine mine(p.rows);
+    if (!mine.live) return;
+    const int part = mine.part, which = mine.which;
+    const uint64_t row = mine.row;
+    float x[kLane];
+    if (!mine.stored) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = 0.0f;
+        for (int e = 0; e < kLane; ++e) x[e] = 0.0f;
     } else {
-        const uint32_t* from = p.rows.codes[which] + row * (kD * BITS / 32) + part * NW;
-        uint32_t words[4];
-        if constexpr (NW == 1) {
-            words[0] = from[0];
-        } else if constexpr (NW == 2) {
-            const u32x2 v = *reinterpret_cast<const u32x2*>(from);
-            words[0] = v[0];
-            words[1] = v[1];
-        } else {
-            const u32x4 v = *reinterpret_cast<const u32x4*>(from);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) words[i] = v[i];
-        }
-        const uint32_t m = p.rows.meta[which][row * (kD / p.rows.group) + part * 16 / p.rows.group];
+        Codes<BITS> c;
+        c.load(p.rows.codes[which] + row * (kD * BITS / 32), part);
+        const uint32_t m = p.rows.meta[which][meta_at(p.rows, row, part)];
         const float s = static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(m & 0xFFFFu)));
         const float z = static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(m >> 16)));
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-            x[e] = fmaf(static_cast<float>((words[e * BITS / 32] >> (e * BITS % 32)) & ((1u << BITS) - 1u)), s, z);
+        for (int e = 0; e < kLane; ++e) x[e] = fmaf(static_cast<float>((c.half[e / PER] >> (e % PER * BITS)) & ((1u << BITS) - 1u)), s, z);
     }
-    store16<DT>(p.x[which] + t * p.st + h * p.sh + part * (16 * ES), x);
+    store8<DT>(p.x[which] + mine.at(p.st, p.sh, kLane * ES), x);
 }
 
 int page_shift(int page_tokens) {
@@ -214,7 +269,7 @@ PagedRows rows_of(const squat_paged_store* s, const int64_t* slots, int64_t n) {
     r.n = n;
     r.n_heads = s->n_kv_heads;
     r.page_shift = page_shift(s->page_tokens);
-    r.group = s->group;
+    r.group_shift = s->group == 32 ? 5 : s->group == 64 ? 6 : 7;
     r.first = 0;
     return r;
 }
