@@ -24,6 +24,7 @@ struct VerifyParams {
     int32_t* accepted;
     int64_t* out;
     double2* sums;                                        // [n_seqs, pieces]: of the residual, of the target's row
+    int32_t* stand;                                       // [n_seqs]: accepted drafts, and in bit 8 whether that is all of them
     int pieces;
 };
 
@@ -62,10 +63,23 @@ __device__ __forceinline__ void entries(const unsigned char* row, int i, int n, 
 
 // How a sequence's drafts end: `accepted` of them, and the rows that the next token comes from (draft: NULL where p itself is meant).
 struct Verdict {
-    int accepted, limit;
+    int accepted;
+    bool all;
     const unsigned char *p, *q;
     int64_t taken;                                        // the draft chosen outright that was refused, or -1
 };
+
+template <int DT>
+__device__ __forceinline__ Verdict rows_after(const VerifyParams& p, int s, int accepted, bool all) {
+    constexpr int ES = DT == SQUAT_F32 ? 4 : 2;
+    Verdict v;
+    v.accepted = accepted;
+    v.all = all;
+    v.p = p.target + (s * p.tss + accepted * p.tsp) * ES;
+    v.q = !all && p.draft ? p.draft + (s * p.dss + accepted * p.dsp) * ES : nullptr;
+    v.taken = !all && !p.draft ? p.tokens[static_cast<int64_t>(s) * p.n_drafts + accepted] : -1;
+    return v;
+}
 
 template <int DT>
 __device__ __forceinline__ Verdict decide(const VerifyParams& p, int s) {
@@ -84,13 +98,8 @@ __device__ __forceinline__ Verdict decide(const VerifyParams& p, int s) {
         refused = !(u * qx < px);
     }
     const uint64_t m = __ballot(refused);
-    Verdict v;
-    v.limit = n;
-    v.accepted = m ? min(__builtin_ctzll(m), n) : n;      // (64 drafts, all accepted: no lane is left to say so)
-    v.p = p.target + (s * p.tss + v.accepted * p.tsp) * ES;
-    v.q = v.accepted < n && p.draft ? p.draft + (s * p.dss + v.accepted * p.dsp) * ES : nullptr;
-    v.taken = v.accepted < n && !p.draft ? p.tokens[static_cast<int64_t>(s) * p.n_drafts + v.accepted] : -1;
-    return v;
+    const int accepted = m ? min(__builtin_ctzll(m), n) : n;        // (64 drafts, all accepted: no lane is left to say so)
+    return rows_after<DT>(p, s, accepted, accepted == n);
 }
 
 // What a lane's entries of the row weigh in the draw of the next token.
@@ -140,119 +149,121 @@ __global__ void __launch_bounds__(kThreads) verify_sums_kernel(const VerifyParam
             t += part[w].y;
         }
         p.sums[static_cast<int64_t>(s) * p.pieces + blockIdx.x] = double2{r, t};
+        if (blockIdx.x == 0) p.stand[s] = v.accepted | (v.all ? 256 : 0);
     }
 }
 
-// The running sum up to and including the thread's x, over the workgroup's threads in order; `all`: over all of them.
-__device__ __forceinline__ double block_scan(double x, double (&lds)[kThreads / 64], double& all) {
-    const int lane = static_cast<int>(threadIdx.x) & 63, wave = static_cast<int>(threadIdx.x) >> 6;
+// The running sum over the wavefront's lanes, up to and including the lane's own.
+__device__ __forceinline__ double wave_scan(double x) {
+    const int lane = static_cast<int>(threadIdx.x) & 63;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
         const double y = __shfl_up(x, o, 64);
         if (lane >= o) x += y;
     }
-    __syncthreads();                                      // (the last round's readers are through)
-    if (lane == 63) lds[wave] = x;
-    __syncthreads();
-    double before = 0.0;
-    all = 0.0;
-    for (int w = 0; w < kThreads / 64; ++w) {
-        if (w < wave) before += lds[w];
-        all += lds[w];
-    }
-    return before + x;
+    return x;
 }
 
+// One workgroup a sequence.  The piece that holds the mark is found by every wavefront for itself; in the piece a thread has kOwn entries in a row.
 template <int DT>
 __global__ void __launch_bounds__(kThreads) verify_pick_kernel(const VerifyParams p) {
-    __shared__ double lds[kThreads / 64];
-    __shared__ int found, fallback;
-    __shared__ double before_found;
-    const int s = static_cast<int>(blockIdx.x), tid = static_cast<int>(threadIdx.x);
-    Verdict v = decide<DT>(p, s);
+    constexpr int kOwn = kPiece / kThreads, kLoads = kOwn / kPer<DT>;
+    __shared__ double ends[kThreads / 64];
+    __shared__ int found[kThreads / 64], last_of[kThreads / 64];
+    const int s = static_cast<int>(blockIdx.x), tid = static_cast<int>(threadIdx.x), lane = tid & 63, wave = tid >> 6;
     const double2* sums = p.sums + static_cast<int64_t>(s) * p.pieces;
-    double total = 0.0, total_p = 0.0, all;
-    for (int c = 0; c < p.pieces; c += kThreads) {        // uniform
-        const double2 x = c + tid < p.pieces ? sums[c + tid] : double2{0.0, 0.0};
-        (void)block_scan(x.x, lds, all);
-        total += all;
-        (void)block_scan(x.y, lds, all);
-        total_p += all;
+    const double u = static_cast<double>(p.u_next[s]);
+    const int stand = p.stand[s];
+    const auto sum_at = [&](int c) { return c + lane < p.pieces ? sums[c + lane] : double2{0.0, 0.0}; };
+    const double2 head = sum_at(0);                       // (64 pieces, 262144 entries: all there is in most cases)
+    double total = head.x, total_p = head.y;
+    for (int c = 64; c < p.pieces; c += 64) {             // uniform
+        const double2 x = sum_at(c);
+        total += x.x;
+        total_p += x.y;
     }
+    total = wave_sum(total);
+    total_p = wave_sum(total_p);
+    Verdict v = rows_after<DT>(p, s, stand & 255, (stand & 256) != 0);
     const bool plain = !(total > 0.0);                    // nothing is left of the residual: the target's own row
     if (plain) {
         total = total_p;
         v.q = nullptr;
         v.taken = -1;
     }
-    const double mark = static_cast<double>(p.u_next[s]) * total;
-    // the piece that holds the mark: the first whose running sum is over it
-    if (tid == 0) {
-        found = 0x7FFFFFFF;
-        fallback = 0;
-        before_found = 0.0;
-    }
+    const double mark = u * total;
+    // the first piece whose running sum is over the mark, and what lies before it; or (a mark that rounding put on the very end) the last
+    // piece that counts
+    int piece = -1, counts = 0;
     double before = 0.0;
-    for (int c = 0; c < p.pieces; c += kThreads) {        // uniform
-        const double2 x = c + tid < p.pieces ? sums[c + tid] : double2{0.0, 0.0};
-        const double mine = plain ? x.y : x.x, upto = before + block_scan(mine, lds, all);
-        if (c + tid < p.pieces && upto > mark) atomicMin(&found, c + tid);
-        if (mine > 0.0) atomicMax(&fallback, c + tid);
-        __syncthreads();
-        if (found < 0x7FFFFFFF) {                         // uniform: everybody is past the barrier
-            if (found == c + tid) before_found = upto - mine;
-            break;
+    for (int c = 0; c < p.pieces && piece < 0; c += 64) { // uniform
+        const double2 x = c == 0 ? head : sum_at(c);
+        const double mine = plain ? x.y : x.x, upto = before + wave_scan(mine);
+        const uint64_t over = __ballot(c + lane < p.pieces && upto > mark), some = __ballot(mine > 0.0);
+        if (some) counts = c + 63 - __builtin_clzll(some);
+        if (over) {
+            const int at = __builtin_ctzll(over);
+            piece = c + at;
+            before = __shfl(upto - mine, at, 64);
+        } else {
+            before = __shfl(upto, 63, 64);
         }
-        before += all;
     }
-    __syncthreads();
-    const bool any = found < 0x7FFFFFFF;
-    const int piece = any ? found : fallback;             // (a mark that rounding put on the very end: the last entry that counts)
-    before = any ? before_found : -INFINITY;
-    __syncthreads();
-    if (tid == 0) {
-        found = 0x7FFFFFFF;
-        fallback = 0;
+    if (piece < 0) {
+        piece = counts;
+        before = -INFINITY;
     }
-    __syncthreads();
-    int first = 0x7FFFFFFF, last = 0;                     // the thread's first entry over the mark, and its last that counts
-    for (int k = 0; k < kPiece / (kThreads * kPer<DT>); ++k) {
-        const int64_t i = static_cast<int64_t>(piece) * kPiece + (k * kThreads + tid) * kPer<DT>;
-        double r[kPer<DT>], t[kPer<DT>], sum = 0.0;
+    const int64_t i0 = static_cast<int64_t>(piece) * kPiece + tid * kOwn;
+    double r[kOwn], sum = 0.0;
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+        double re[kPer<DT>], te[kPer<DT>];
+        const int64_t i = i0 + k * kPer<DT>;
         if (i < p.vocab) {
-            weights<DT>(v, static_cast<int>(i), p.vocab, r, t);
+            weights<DT>(v, static_cast<int>(i), p.vocab, re, te);
         } else {
 #pragma unroll
-            for (int e = 0; e < kPer<DT>; ++e) r[e] = 0.0;
+            for (int e = 0; e < kPer<DT>; ++e) re[e] = 0.0;
         }
-#pragma unroll
-        for (int e = 0; e < kPer<DT>; ++e) sum += r[e];
-        double run = before + (block_scan(sum, lds, all) - sum);
 #pragma unroll
         for (int e = 0; e < kPer<DT>; ++e) {
-            run += r[e];
-            if (r[e] > 0.0) {
-                last = static_cast<int>(i) + e;
-                if (run > mark) first = min(first, last);
-            }
+            r[k * kPer<DT> + e] = re[e];
+            sum += re[e];
         }
-        before += all;
+    }
+    const double upto = wave_scan(sum);
+    if (lane == 63) ends[wave] = upto;
+    __syncthreads();
+    double run = before + (upto - sum);
+    for (int w = 0; w < wave; ++w) run += ends[w];
+    int first = 0x7FFFFFFF, last = -1;                    // the thread's first entry over the mark, and its last that counts
+#pragma unroll
+    for (int e = 0; e < kOwn; ++e) {
+        run += r[e];
+        if (r[e] > 0.0) {
+            last = static_cast<int>(i0) + e;
+            if (run > mark) first = min(first, last);
+        }
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
         first = min(first, __shfl_xor(first, o, 64));
         last = max(last, __shfl_xor(last, o, 64));
     }
-    if ((tid & 63) == 0) {
-        atomicMin(&found, first);
-        atomicMax(&fallback, last);
+    if (lane == 0) {
+        found[wave] = first;
+        last_of[wave] = last;
     }
     __syncthreads();
-    const int picked = found < 0x7FFFFFFF ? found : fallback;
-    if (tid <= p.n_drafts) {
-        const int64_t x = tid < v.accepted ? p.tokens[static_cast<int64_t>(s) * p.n_drafts + tid] : (tid == v.accepted ? picked : -1);
-        p.out[static_cast<int64_t>(s) * (p.n_drafts + 1) + tid] = x;
+    if (tid > p.n_drafts && tid > 0) return;
+#pragma unroll
+    for (int w = 0; w < kThreads / 64; ++w) {
+        first = w == 0 ? found[0] : min(first, found[w]);
+        last = w == 0 ? last_of[0] : max(last, last_of[w]);
     }
+    const int picked = first < 0x7FFFFFFF ? first : max(last, 0);
+    const int64_t x = tid < v.accepted ? p.tokens[static_cast<int64_t>(s) * p.n_drafts + tid] : (tid == v.accepted ? picked : -1);
+    p.out[static_cast<int64_t>(s) * (p.n_drafts + 1) + tid] = x;
     if (tid == 0) p.accepted[s] = v.accepted;
 }
 
@@ -271,7 +282,7 @@ bool sizes_ok(int n_seqs, int64_t vocab) { return n_seqs >= 0 && n_seqs <= 65535
 
 extern "C" size_t squat_verify_drafts_workspace(int n_seqs, int64_t vocab) {
     if (!sizes_ok(n_seqs, vocab)) return 0;
-    return static_cast<size_t>(n_seqs) * ((vocab + kPiece - 1) / kPiece) * sizeof(double2);
+    return static_cast<size_t>(n_seqs) * (((vocab + kPiece - 1) / kPiece) * sizeof(double2) + sizeof(int32_t));
 }
 
 extern "C" int squat_verify_drafts(const int64_t* tokens, int n_seqs, int n_drafts, int64_t vocab, const void* target,
@@ -308,6 +319,7 @@ extern "C" int squat_verify_drafts(const int64_t* tokens, int n_seqs, int n_draf
     p.out = out;
     p.sums = static_cast<double2*>(ws);
     p.pieces = static_cast<int>((vocab + kPiece - 1) / kPiece);
+    p.stand = reinterpret_cast<int32_t*>(p.sums + static_cast<int64_t>(n_seqs) * p.pieces);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     switch (dt) {
         case SQUAT_F32: return launch_verify<SQUAT_F32>(s, p);
