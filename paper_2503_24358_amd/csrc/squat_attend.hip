@@ -76,7 +76,7 @@ struct Tile {
     int row0;                                             // first row of the tile
     int pos0;                                             // position of the first new token
     int end;                                              // tokens that the tile's last row sees
-    int steps, span, parts;                               // of kStep tokens: in all, in a part
+    int steps, span, parts;                               // of kStep tokens: in all, in a part (an even number)
 };
 
 // Tile w of a launch: the first R rows of sequence w, or, from w = n_seqs on, further ones: sequence s has the numbers n_seqs + floor(q_start[s] qpk /
@@ -115,7 +115,7 @@ __device__ __forceinline__ bool find_tile(const AttendParams& p, int w, Tile& t)
     t.end = min(max(t.pos0 + (min(t.row0 + R, t.rows) - 1) / p.qpk + 1, 0), len);
     t.steps = (t.end + kStep - 1) / kStep;
     t.span = p.span;
-    if (t.steps > p.span * p.splits) t.span = (t.steps + p.splits - 1) / p.splits;
+    if (t.steps > p.span * p.splits) t.span = ((t.steps + p.splits - 1) / p.splits + 1) & ~1;
     t.parts = max((t.steps + t.span - 1) / t.span, 1);
     return true;
 }
@@ -895,6 +895,330 @@ __global__ void __launch_bounds__(256) attend_few_kernel(const AttendParams p) {
     if (r < R) finish_row<R, QDT, R>(p, t, work, r, sums, stats, r);
 }
 
+// Many rows of bf16 queries (a chunk of a prompt): bound by the products, so that what a code costs is shared by more rows.  A workgroup meets 128
+// rows, 32 a wavefront, with steps of 64 tokens that its wavefronts dequantize into LDS for all four: the first two a half's values each, as the
+// second product's operands in a row, the others a half's keys, 16 bytes more than their channels a row, which keeps 16 rows on different
+// banks.  Two places for steps: one is filled from registers, loaded a step before, while the other is met; one barrier a step.
+// Keys are rounded to fp16 here (2^-11), so this is for results of bf16; rows below kChunkRows a sequence keep the exact form.
+constexpr int kChunkRows = 2048, kChunkTile = 128, kChunkStep = 64, kKeyPitch = 2 * kD + 16;
+
+// Which channel element e of a key's unit of 8 is (see code_pair: a word's halves are unpacked together).
+template <int BITS>
+__device__ __forceinline__ constexpr int unit_channel(int unit, int e) {
+    return BITS == 2 ? 16 * (unit >> 1) + 4 * (unit & 1) + (e >> 1) + 8 * (e & 1) : BITS == 4 ? 8 * unit + (e >> 1) + 4 * (e & 1) : 8 * unit + e;
+}
+
+template <int BITS, int NG>
+__global__ void __launch_bounds__(256, 2) attend_chunk_kernel(const AttendParams p) {
+    constexpr int R = kChunkTile, NQ = 2;
+    constexpr int ROW = kD * BITS / 8, MROW = 4 * NG;     // bytes of a token's codes, and of its scales and zero-points
+    __shared__ __align__(16) unsigned char keys[2][kChunkStep * kKeyPitch];
+    __shared__ __align__(16) unsigned char values[2][2][8][1024];
+    __shared__ int spoilt[2][2];                          // a half's values hold a scale or zero-point that is not finite,
+    __shared__ int missing[2][2];                         // or one of its pages does not exist
+    const Work work(p);
+    const int part = work.part, kvh = work.kvh;
+    Tile t;
+    if (!find_tile<R>(p, work.tile, t) || part >= t.parts) return;
+    const int lane = static_cast<int>(threadIdx.x) & 63, m = lane & 15, h = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+    const int first = part * t.span / 2, last = (min((part + 1) * t.span, t.steps) + 1) / 2;      // of 64 tokens (spans are even)
+    const Walk walk(p, t, kvh);
+    const int least_seen = t.pos0 + t.row0 / p.qpk;       // every row of the tile sees this token and all before it
+    const Places places_ = places<BITS>();
+    const half2v bias = {static_cast<_Float16>(Bias<BITS>::value), static_cast<_Float16>(Bias<BITS>::value)};
+
+    // What this wavefront dequantizes: half wave & 1 of a step.
+    const bool of_keys = wave >= 2;                       // uniform
+    const int half = wave & 1;
+    constexpr int KW = ROW / 8;                           // words of half a key: a lane's
+    uint32_t kw[KW], km[NG == 4 ? 2 : 1];
+    ValueWord<BITS> vw[2][4];
+    uint32_t vm[2][4];
+    int limit[2];
+    const int key_row = lane >> 1, key_half = lane & 1;
+    Pages ahead = walk.pages(2 * first + half);
+    const auto load = [&](int step) {                     // of 64 tokens; `ahead` are its pages, and then the next one's
+        const Place a = walk.place(2 * step + half, ahead);
+        ahead = walk.pages(2 * step + 2 + half);
+        limit[0] = a.limit[0];
+        limit[1] = a.limit[1];
+        if (of_keys) {
+            const uint64_t row = (key_row < 16 ? a.rows[0] : a.rows[1]) + (key_row & 15);
+            const unsigned char* codes = p.kc + row * ROW + key_half * (ROW / 2);
+#pragma unroll
+            for (int i = 0; i < KW / 4; ++i) {
+                const u32x4 x = *reinterpret_cast<const u32x4*>(codes + 16 * i);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) kw[4 * i + k] = x[k];
+            }
+            const unsigned char* meta = p.km + row * MROW;
+            if constexpr (NG == 4) {
+                const u32x2 x = *reinterpret_cast<const u32x2*>(meta + 8 * key_half);
+                km[0] = x[0];
+                km[1] = x[1];
+            } else {
+                km[0] = *reinterpret_cast<const uint32_t*>(meta + (NG == 2 ? 4 * key_half : 0));
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const unsigned char *codes = p.vc + (a.rows[u] + 4 * h) * ROW + m * BITS, *meta = p.vm + (a.rows[u] + 4 * h) * MROW + 4 * ((m * NG) >> 4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    vw[u][i].w = *reinterpret_cast<const decltype(vw[u][i].w)*>(codes + i * ROW);
+                    vm[u][i] = *reinterpret_cast<const uint32_t*>(meta + i * MROW);
+                }
+            }
+        }
+    };
+    const auto dequantize = [&](int step, int place) {
+        if (of_keys) {
+            unsigned char* to = keys[place] + (32 * half + key_row) * kKeyPitch + key_half * kD;
+            half2v ks[NG == 4 ? 2 : 1], kz[NG == 4 ? 2 : 1];
+#pragma unroll
+            for (int g = 0; g < (NG == 4 ? 2 : 1); ++g) {
+                const half2v sz = as_half2(km[g]), odd = sz * half2v{static_cast<_Float16>(0.0f), static_cast<_Float16>(0.0f)};
+                const _Float16 zero = sz[1] + (odd[0] + odd[1]);              // (metadata that is not finite: NaN)
+                ks[g] = half2v{sz[0], sz[0]};
+                kz[g] = half2v{zero, zero};
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {                 // units of 8 channels
+                const int g = NG == 4 ? k >> 2 : 0;
+                u32x4 y;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    uint32_t x;
+                    if constexpr (BITS == 2) x = code_pair<2>(kw[k >> 1], 8 * (k & 1) + 2 * r, places_);
+                    else if constexpr (BITS == 4) x = code_pair<4>(kw[k], 4 * r, places_);
+                    else x = byte_perm(places_.bias, kw[2 * k + (r >> 1)], (r & 1) ? 0x05030502u : 0x05010500u);
+                    y[r] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(as_half2(x) - bias, ks[g], kz[g]));
+                }
+                *reinterpret_cast<u32x4*>(to + 16 * k) = y;
+            }
+        } else {
+            const int t0 = step * kChunkStep + 32 * half;
+            bool odd = false;
+            if (t0 + 32 > least_seen + 1 || t0 + 16 > limit[0] || t0 + 32 > limit[1]) {           // uniform
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const bool there = t0 + 16 * u + 4 * h + i < limit[u];
+                        odd |= there && not_finite(vm[u][i]);
+                        if (!there || not_finite(vm[u][i])) vm[u][i] = 0u;
+                    }
+            }
+            const uint64_t any = __ballot(odd);
+            if (lane == 0) {
+                spoilt[place][half] = any != 0;
+                missing[place][half] = limit[0] == 0 || limit[1] == 0;
+            }
+            half2v vs[4], vz[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t a = vm[e >> 1][2 * (e & 1)], b = vm[e >> 1][2 * (e & 1) + 1];
+                vs[e] = as_half2(byte_perm(b, a, 0x05040100u));
+                vz[e] = as_half2(byte_perm(b, a, 0x07060302u));
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                u32x4 y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    y[e] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(as_half2(value_pair<BITS>(vw[e >> 1][2 * (e & 1)], vw[e >> 1][2 * (e & 1) + 1], j, places_)) - bias,
+                                                                                  vs[e], vz[e]));
+                *reinterpret_cast<u32x4*>(values[place][half][j] + 16 * lane) = y;
+            }
+        }
+    };
+    if (first < last) load(first);
+
+    // The queries, a lane's 8 channels of each 32, in the keys' order, times a power of two that brings a row's largest element into [1/2, 1).
+    half8 qf[NQ][4];
+    float scale[NQ], slack[NQ];
+    int seen[NQ];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        const int row = t.row0 + 32 * wave + 16 * n + m;
+        const bool live = row < t.rows;
+        const int r = live ? row : t.rows - 1;
+        const int i = r / p.qpk, hq = kvh * p.qpk + (r - i * p.qpk);
+        seen[n] = live ? t.pos0 + i : -1;
+        const unsigned char* src = p.q + ((t.start + i) * p.qst + hq * p.qsh) * 2;
+        uint32_t raw[4][4], big = 0u;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const int unit = 4 * s + h;
+            if constexpr (BITS == 2) {
+                const u32x2 a = *reinterpret_cast<const u32x2*>(src + 2 * unit_channel<2>(unit, 0)), b = *reinterpret_cast<const u32x2*>(src + 2 * unit_channel<2>(unit, 1));
+                raw[s][0] = a[0];
+                raw[s][1] = a[1];
+                raw[s][2] = b[0];
+                raw[s][3] = b[1];
+            } else {
+                const u32x4 a = *reinterpret_cast<const u32x4*>(src + 16 * unit);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) raw[s][k] = a[k];
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) big = max_halves(big, raw[s][k] & 0x7FFF7FFFu);
+        }
+        big = max(big & 0xFFFFu, big >> 16);
+        big = max(big, static_cast<uint32_t>(__shfl_xor(static_cast<int>(big), 16, 64)));
+        big = max(big, static_cast<uint32_t>(__shfl_xor(static_cast<int>(big), 32, 64)));
+        const float largest = as_f32(big << 16);
+        int e2 = 0;
+        if (largest > 0.0f && largest < INFINITY) (void)frexpf(largest, &e2);
+        e2 = max(-100, min(100, e2));
+        const float factor = ldexpf(p.scale < 0.0f ? -1.0f : 1.0f, -e2);
+        scale[n] = fmaxf(ldexpf(fabsf(p.scale), e2), 1e-30f);
+        slack[n] = kSlack / scale[n];
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int c = BITS == 8 ? e : (e >> 1) + 4 * (e & 1);         // of the lane's 8, as loaded
+                const uint32_t x = raw[s][c >> 1];
+                qf[n][s][e] = live ? static_cast<_Float16>(as_f32((c & 1) ? (x & 0xFFFF0000u) : (x << 16)) * factor) : static_cast<_Float16>(0.0f);
+            }
+    }
+
+    f32x4 o[NQ][8], total[NQ];                            // O^T: channels 8 (4 h + i) + j, column m; the weights' sum
+    float top[NQ];
+    half8 ones;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ones[e] = static_cast<_Float16>(1.0f);
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        top[n] = -INFINITY;
+        total[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[n][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    if (first < last) {
+        dequantize(first, 0);
+        if (first + 1 < last) load(first + 1);
+    }
+    __syncthreads();
+
+    for (int step = first; step < last; ++step) {
+        const int place = (step - first) & 1;
+        if (step + 1 < last) {
+            dequantize(step + 1, place ^ 1);
+            if (step + 2 < last) load(step + 2);
+        }
+#pragma unroll
+        for (int part_of = 0; part_of < 2; ++part_of) {
+            const int t0 = step * kChunkStep + 32 * part_of;
+            float x[NQ][2][4];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const unsigned char* from = keys[place] + (32 * part_of + 16 * u + m) * kKeyPitch + 16 * h;
+                f32x4 a[NQ];
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) a[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    const half8 kf = *reinterpret_cast<const half8*>(from + 64 * s);
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) a[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[n][s], a[n], 0, 0, 0);
+                }
+#pragma unroll
+                for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[n][u][i] = a[n][i];
+            }
+            if (t0 + 32 > least_seen + 1 || t0 + 32 > t.end || missing[place][part_of]) {         // uniform
+                const Place here = walk.place(2 * step + part_of, walk.pages(2 * step + part_of));
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int token = t0 + 16 * u + 4 * h + i;
+#pragma unroll
+                        for (int n = 0; n < NQ; ++n)
+                            if (token >= here.limit[u] || token > seen[n]) x[n][u][i] = -INFINITY;
+                    }
+                if (spoilt[place][part_of]) {             // a token that only some rows see spoils those alone
+#pragma unroll 1
+                    for (int k = 0; k < 32; ++k) {
+                        if (t0 + k >= (k < 16 ? here.limit[0] : here.limit[1])) continue;
+                        const uint64_t row = (k < 16 ? here.rows[0] : here.rows[1]) + (k & 15);
+                        const uint32_t meta = *reinterpret_cast<const uint32_t*>(p.vm + row * MROW + 4 * ((h * NG) >> 2));
+#pragma unroll
+                        for (int n = 0; n < NQ; ++n) {
+                            const float add = not_finite(meta) && t0 + k <= seen[n] ? NAN : 0.0f;
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) o[n][j] += add;
+                        }
+                    }
+                }
+            }
+            half8 pf[NQ];
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                float most = x[n][0][0];
+#pragma unroll
+                for (int e = 1; e < 8; ++e) most = fmaxf(most, x[n][e >> 2][e & 3]);
+                if (__ballot(most > top[n] + slack[n])) {
+                    most = fmaxf(most, __shfl_xor(most, 16, 64));
+                    most = fmaxf(most, __shfl_xor(most, 32, 64));
+                    const float now = fmaxf(top[n], most);
+                    const float by = now > -INFINITY ? __builtin_amdgcn_exp2f((top[n] - now) * scale[n]) : 1.0f;
+                    top[n] = now;
+                    total[n] *= by;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) o[n][j] *= by;
+                }
+                const float from = top[n] > -INFINITY ? kLift - top[n] * scale[n] : 0.0f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) pf[n][e] = static_cast<_Float16>(__builtin_amdgcn_exp2f(fmaf(x[n][e >> 2][e & 3], scale[n], from)));
+                total[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pf[n], total[n], 0, 0, 0);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const half8 vf = *reinterpret_cast<const half8*>(values[place][part_of][j] + 16 * lane);
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) o[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[n], o[n][j], 0, 0, 0);
+            }
+        }
+        __syncthreads();
+    }
+
+    // a wavefront's rows are its own: 8 channels a piece from a lane's sums
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        const int r = 32 * wave + 16 * n + m, row = t.row0 + r;
+        if (row >= t.rows) continue;
+        const float sum = total[n][0], stat = top[n] > -INFINITY ? top[n] * scale[n] : -INFINITY;
+        if (p.splits > 1) {
+            const int64_t to_row = ((static_cast<int64_t>(part) * p.n_tiles + work.tile) * p.n_kv + kvh) * R + r;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float* to = p.part_o + to_row * kD + 8 * (4 * h + i);
+                *reinterpret_cast<f32x4*>(to) = f32x4{o[n][0][i], o[n][1][i], o[n][2][i], o[n][3][i]};
+                *reinterpret_cast<f32x4*>(to + 4) = f32x4{o[n][4][i], o[n][5][i], o[n][6][i], o[n][7][i]};
+            }
+            if (h == 0) p.part_ml[to_row] = float2{stat, sum};
+            continue;
+        }
+        const int i0 = row / p.qpk, hq = kvh * p.qpk + (row - i0 * p.qpk);
+        const float by = sum == 0.0f ? 1.0f : 1.0f / sum;
+        unsigned char* to = p.out + ((t.start + i0) * p.ost + hq * p.osh) * 2;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            bf16x8 v;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = static_cast<__bf16>(o[n][j][i] * by);
+            *reinterpret_cast<bf16x8*>(to + 16 * (4 * h + i)) = v;
+        }
+        if (p.lse && h == 0)
+            p.lse[static_cast<int64_t>(t.start + i0) * p.n_kv * p.qpk + hq] = sum == 0.0f ? -INFINITY : kLn2 * ((stat - kLift) + __builtin_amdgcn_logf(sum));
+    }
+}
+
 // The parts of a row put together: half a wavefront a part (16 bytes a lane), WAVES wavefronts a row, so that for WAVES = 4 a row's first 128
 // parts are asked for at once; what the parts weigh is asked for with them.
 template <int R, int WAVES, int QDT>
@@ -976,7 +1300,8 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const AttendParams p) 
 }
 
 struct Plan {
-    int nq, rows;                                         // row tiles: of 16 nq rows, or (nq = 0) of a few
+    int nq, rows;                                         // row tiles: of 16 nq rows, or (nq = 0) of a few,
+    bool chunk;                                           // or of a chunk
     int64_t tiles;
     int splits, span;
     size_t o_bytes, ml_bytes;
@@ -984,14 +1309,15 @@ struct Plan {
 
 size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
-Plan plan_attend(const squat_paged_store* s, int n_seqs, int64_t n_new, int q_per_kv, int pages_per_seq, int64_t max_new, int64_t max_kv) {
+Plan plan_attend(const squat_paged_store* s, squat_dtype dt, int n_seqs, int64_t n_new, int q_per_kv, int pages_per_seq, int64_t max_new, int64_t max_kv) {
     Plan a;
     const int64_t room = static_cast<int64_t>(pages_per_seq) * s->page_tokens;
     if (max_new < 1 || max_new > n_new) max_new = n_new;
     if (max_kv < 1 || max_kv > room) max_kv = room;
     const int few = s->group / 8;                         // 16 columns, 128 / group of them a row
     a.nq = max_new * q_per_kv <= few ? 0 : max_new * q_per_kv <= 16 ? 1 : 2;
-    a.rows = a.nq == 0 ? few : 16 * a.nq;
+    a.chunk = dt == SQUAT_BF16 && max_new * q_per_kv >= kChunkRows;
+    a.rows = a.chunk ? kChunkTile : a.nq == 0 ? few : 16 * a.nq;
     a.tiles = n_new * q_per_kv / a.rows + n_seqs;
     // tiles with work: what the hints allow
     int64_t busy = n_seqs * ((max_new * q_per_kv + a.rows - 1) / a.rows);
@@ -1006,7 +1332,7 @@ Plan plan_attend(const squat_paged_store* s, int n_seqs, int64_t n_new, int q_pe
     n = a.rows > room_for ? 1 : n > room_for ? room_for : n;
     a.splits = n < 1 ? 1 : static_cast<int>(n);
     a.span = static_cast<int>((steps + a.splits - 1) / a.splits);
-    a.span = a.span < 1 ? 1 : a.span;
+    a.span = a.span < 1 ? 2 : (a.span + 1) & ~1;          // (whole steps of 64 tokens, for chunks)
     const size_t all = a.splits > 1 ? static_cast<size_t>(a.splits) * a.tiles * s->n_kv_heads * a.rows : 0;
     a.o_bytes = up256(all * kD * sizeof(float));
     a.ml_bytes = up256(all * sizeof(float2));
@@ -1033,17 +1359,18 @@ void launch_few(squat_dtype dt, dim3 grid, hipStream_t s, const AttendParams& p)
     else hipLaunchKernelGGL((attend_few_kernel<BITS, NG, SQUAT_BF16>), grid, dim3(256), 0, s, p);
 }
 template <int BITS, int NG>
-void launch_groups(int nq, squat_dtype dt, dim3 grid, hipStream_t s, const AttendParams& p) {
-    if (nq == 0) launch_few<BITS, NG>(dt, grid, s, p);
-    else if (nq == 1) launch_rows<BITS, NG, 1>(dt, grid, s, p);
-    else launch_rows<BITS, NG, 2>(dt, grid, s, p);
+void launch_groups(int rows, squat_dtype dt, dim3 grid, hipStream_t s, const AttendParams& p) {
+    if (rows == 0) launch_few<BITS, NG>(dt, grid, s, p);
+    else if (rows == 16) launch_rows<BITS, NG, 1>(dt, grid, s, p);
+    else if (rows == 32) launch_rows<BITS, NG, 2>(dt, grid, s, p);
+    else hipLaunchKernelGGL((attend_chunk_kernel<BITS, NG>), grid, dim3(256), 0, s, p);
 }
 template <int BITS>
-void launch_bits(int group, int nq, squat_dtype dt, dim3 grid, hipStream_t s, const AttendParams& p) {
+void launch_bits(int group, int rows, squat_dtype dt, dim3 grid, hipStream_t s, const AttendParams& p) {
     switch (group) {
-        case 32: launch_groups<BITS, 4>(nq, dt, grid, s, p); break;
-        case 64: launch_groups<BITS, 2>(nq, dt, grid, s, p); break;
-        default: launch_groups<BITS, 1>(nq, dt, grid, s, p); break;
+        case 32: launch_groups<BITS, 4>(rows, dt, grid, s, p); break;
+        case 64: launch_groups<BITS, 2>(rows, dt, grid, s, p); break;
+        default: launch_groups<BITS, 1>(rows, dt, grid, s, p); break;
     }
 }
 // A wavefront a row where there are few parts, four where there are many.
@@ -1065,8 +1392,12 @@ void launch_join(squat_dtype dt, unsigned tiles, hipStream_t s, const AttendPara
 extern "C" size_t squat_paged_attention_workspace(const squat_paged_store* store, int n_seqs, int64_t n_new, int q_per_kv,
                                                   int pages_per_seq, int64_t max_new, int64_t max_kv) {
     if (check_store(store) || check_sizes(store, n_seqs, n_new, q_per_kv, pages_per_seq) || n_seqs == 0 || n_new == 0) return 0;
-    const Plan a = plan_attend(store, n_seqs, n_new, q_per_kv, pages_per_seq, max_new, max_kv);
-    return a.o_bytes + a.ml_bytes;
+    size_t most = 0;                                      // (whichever dtype the queries have)
+    for (const squat_dtype dt : {SQUAT_F16, SQUAT_BF16}) {
+        const Plan a = plan_attend(store, dt, n_seqs, n_new, q_per_kv, pages_per_seq, max_new, max_kv);
+        most = a.o_bytes + a.ml_bytes > most ? a.o_bytes + a.ml_bytes : most;
+    }
+    return most;
 }
 
 extern "C" int squat_paged_attention(const squat_paged_store* store, const void* q, squat_dtype q_dt, int64_t n_new, int q_per_kv,
@@ -1087,7 +1418,7 @@ extern "C" int squat_paged_attention(const squat_paged_store* store, const void*
     if (!q || !q_start || !kv_len || !out || (!pages && pages_per_seq > 0)) return SQUAT_E_NULLPTR;
     if (!aligned(q, 16) || !aligned(out, 16) || !aligned(q_start, 4) || !aligned(kv_len, 4) || !aligned(pages, 4) || !aligned(lse, 4))
         return SQUAT_E_ALIGN;
-    const Plan a = plan_attend(store, n_seqs, n_new, q_per_kv, pages_per_seq, max_new, max_kv);
+    const Plan a = plan_attend(store, q_dt, n_seqs, n_new, q_per_kv, pages_per_seq, max_new, max_kv);
     if (a.splits > 1) {
         if (!ws || ws_bytes < a.o_bytes + a.ml_bytes) return SQUAT_E_WORKSPACE;
         if (!aligned(ws, 256)) return SQUAT_E_ALIGN;
@@ -1125,10 +1456,11 @@ extern "C" int squat_paged_attention(const squat_paged_store* store, const void*
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const unsigned gx = static_cast<unsigned>(a.tiles * store->n_kv_heads);
     const dim3 grid(gx * static_cast<unsigned>(a.splits));
+    const int rows = a.chunk ? kChunkTile : 16 * a.nq;
     switch (store->bits) {
-        case 2: launch_bits<2>(store->group, a.nq, q_dt, grid, s, p); break;
-        case 4: launch_bits<4>(store->group, a.nq, q_dt, grid, s, p); break;
-        default: launch_bits<8>(store->group, a.nq, q_dt, grid, s, p); break;
+        case 2: launch_bits<2>(store->group, rows, q_dt, grid, s, p); break;
+        case 4: launch_bits<4>(store->group, rows, q_dt, grid, s, p); break;
+        default: launch_bits<8>(store->group, rows, q_dt, grid, s, p); break;
     }
     rc = check_launch();
     if (rc || a.splits == 1) return rc;
@@ -1136,7 +1468,8 @@ extern "C" int squat_paged_attention(const squat_paged_store* store, const void*
         case 4: launch_join<4>(q_dt, gx, s, p); break;
         case 8: launch_join<8>(q_dt, gx, s, p); break;
         case 16: launch_join<16>(q_dt, gx, s, p); break;
-        default: launch_join<32>(q_dt, gx, s, p); break;
+        case 32: launch_join<32>(q_dt, gx, s, p); break;
+        default: launch_join<kChunkTile>(q_dt, gx, s, p); break;
     }
     return check_launch();
 }

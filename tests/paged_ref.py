@@ -64,9 +64,9 @@ def lists(rng, lens, page, n_pages, width=None):
     return table
 
 
-def attention(q, store, bits, table, lens, starts, out_scale):
+def attention(q, store, bits, table, lens, starts, out_scale, rounded_keys=False):
     """(out, lse, sum p |v|, and the bound's logit error) in float64.  q [n, Hq, 128] float64; store (kc, km, vc, vm) numpy.  A page number
-    outside the store: its tokens are seen by nobody."""
+    outside the store: its tokens are seen by nobody.  rounded_keys: the keys enter rounded to fp16, 2^-11 of each product."""
     kc, km, vc, vm = store
     n_pages, heads, page = kc.shape[:3]
     qpk = q.shape[1] // heads
@@ -95,6 +95,8 @@ def attention(q, store, bits, table, lens, starts, out_scale):
                     mass[a + i, j] = p @ np.abs(v[seen])
                     # a logit: 128 products summed in fp32 from the bias on, then a handful of operations a group
                     off[a + i, j] = abs(out_scale) * (size[seen] @ np.abs(q[a + i, j])).max() * 40 * 2.0 ** -24 + np.abs(x).max() * 2.0 ** -22
+                    if rounded_keys:
+                        off[a + i, j] += abs(out_scale) * (np.abs(k[seen]) @ np.abs(q[a + i, j])).max() * 2.0 ** -11
     return out, lse, mass, off
 
 
