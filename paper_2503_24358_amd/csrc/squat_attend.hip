@@ -76,7 +76,7 @@ struct Tile {
     int row0;                                             // first row of the tile
     int pos0;                                             // position of the first new token
     int end;                                              // tokens that the tile's last row sees
-    int steps, span, parts;                               // of kStep tokens: in all, in a part (a multiple of 4)
+    int steps, span, parts;                               // of kStep tokens: in all, in a part
 };
 
 // Tile w of a launch: the first R rows of sequence w, or, from w = n_seqs on, further ones: sequence s has the numbers n_seqs + floor(q_start[s] qpk /
@@ -115,7 +115,7 @@ __device__ __forceinline__ bool find_tile(const AttendParams& p, int w, Tile& t)
     t.end = min(max(t.pos0 + (min(t.row0 + R, t.rows) - 1) / p.qpk + 1, 0), len);
     t.steps = (t.end + kStep - 1) / kStep;
     t.span = p.span;
-    if (t.steps > p.span * p.splits) t.span = ((t.steps + p.splits - 1) / p.splits + 3) & ~3;
+    if (t.steps > p.span * p.splits) t.span = (t.steps + p.splits - 1) / p.splits;
     t.parts = max((t.steps + t.span - 1) / t.span, 1);
     return true;
 }
@@ -902,7 +902,9 @@ __global__ void __launch_bounds__(256) attend_few_kernel(const AttendParams p) {
 // while the other is met; one barrier a step.  A SIMD has a wavefront of each kind, and they dequantize at different quarters of a step, so that
 // one's vector instructions run beside the other's products.  2048 new tokens over 16384, 4 query heads, 8 KV heads, 4 bits: 592 us, 870 TFLOP/s
 // (four wavefronts and 64 tokens a step, two workgroups a compute unit: 701; without the values' operands in front of the weights 622).
-// Keys are rounded to fp16 here (2^-11), so this is for results of bf16; rows below kChunkRows a sequence keep the exact form.
+// Keys are rounded to fp16 here (2^-11), so this is for results of bf16, for chunks of at least kChunkRows rows and for calls that give half of the compute units a tile, which meets its
+// sequence in one part.  (us, this | the exact form, 4 query heads, 4 bits: 8 sequences of 512 new tokens to 2048, 512 tiles, 226 | 278; 4 of 512,
+// whole prompts, 256 tiles, 42 | 49; 8 of 256 new, 1024 rows, 160 | 159; in parts, 1 of 512 to 32768, 64 tiles, 598 | 539.)
 constexpr int kChunkRows = 2048, kChunkTile = 256, kChunkStep = 128, kChunkWaves = 8, kKeyPitch = 2 * kD + 16;
 
 // Which channel element e of a key's unit of 8 is (see code_pair: a word's halves are unpacked together).
@@ -920,12 +922,12 @@ __global__ void __launch_bounds__(64 * kChunkWaves, 2) attend_chunk_kernel(const
     __shared__ int spoilt[2][4];                          // a quarter's values hold a scale or zero-point that is not finite,
     __shared__ int missing[2][4];                         // or one of its pages does not exist
     const Work work(p);
-    const int part = work.part, kvh = work.kvh;
+    const int kvh = work.kvh;
     Tile t;
-    if (!find_tile<R>(p, work.tile, t) || part >= t.parts) return;
+    if (!find_tile<R>(p, work.tile, t)) return;
     const int lane = static_cast<int>(threadIdx.x) & 63, m = lane & 15, h = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
-    const int first = part * t.span / 4, last = (min((part + 1) * t.span, t.steps) + 3) / 4;      // of 128 tokens (spans are whole ones)
+    const int last = (t.steps + 3) / 4;                   // steps of 128 tokens
     const Walk walk(p, t, kvh);
     const int least_seen = t.pos0 + t.row0 / p.qpk;       // every row of the tile sees this token and all before it
     const Places places_ = places<BITS>();
@@ -940,7 +942,7 @@ __global__ void __launch_bounds__(64 * kChunkWaves, 2) attend_chunk_kernel(const
     uint32_t vm[2][4];
     int limit[2];
     const int key_row = lane >> 1, key_half = lane & 1;
-    Pages ahead = walk.pages(4 * first + quarter);
+    Pages ahead = walk.pages(quarter);
     const auto load = [&](int step) {                     // of 128 tokens; `ahead` are its pages, and then the next one's
         const Place a = walk.place(4 * step + quarter, ahead);
         ahead = walk.pages(4 * step + 4 + quarter);
@@ -1036,7 +1038,7 @@ __global__ void __launch_bounds__(64 * kChunkWaves, 2) attend_chunk_kernel(const
             }
         }
     };
-    if (first < last) load(first);
+    if (last > 0) load(0);
 
     // The queries, a lane's 8 channels of each 32, in the keys' order, times a power of two that brings a row's largest element into [1/2, 1).
     half8 qf[NQ][4];
@@ -1100,14 +1102,14 @@ __global__ void __launch_bounds__(64 * kChunkWaves, 2) attend_chunk_kernel(const
 #pragma unroll
         for (int j = 0; j < 8; ++j) o[n][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
-    if (first < last) {
-        dequantize(first, 0);
-        if (first + 1 < last) load(first + 1);
+    if (last > 0) {
+        dequantize(0, 0);
+        if (last > 1) load(1);
     }
     __syncthreads();
 
-    for (int step = first; step < last; ++step) {
-        const int place = (step - first) & 1;
+    for (int step = 0; step < last; ++step) {
+        const int place = step & 1;
 #pragma unroll 1
         for (int part_of = 0; part_of < 4; ++part_of) {
             if (part_of == (of_keys ? 2 : 0) && step + 1 < last) {            // uniform
@@ -1199,17 +1201,6 @@ __global__ void __launch_bounds__(64 * kChunkWaves, 2) attend_chunk_kernel(const
         const int r = 32 * wave + 16 * n + m, row = t.row0 + r;
         if (row >= t.rows) continue;
         const float sum = total[n][0], stat = top[n] > -INFINITY ? top[n] * scale[n] : -INFINITY;
-        if (p.splits > 1) {
-            const int64_t to_row = ((static_cast<int64_t>(part) * p.n_tiles + work.tile) * p.n_kv + kvh) * R + r;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float* to = p.part_o + to_row * kD + 8 * (4 * h + i);
-                *reinterpret_cast<f32x4*>(to) = f32x4{o[n][0][i], o[n][1][i], o[n][2][i], o[n][3][i]};
-                *reinterpret_cast<f32x4*>(to + 4) = f32x4{o[n][4][i], o[n][5][i], o[n][6][i], o[n][7][i]};
-            }
-            if (h == 0) p.part_ml[to_row] = float2{stat, sum};
-            continue;
-        }
         const int i0 = row / p.qpk, hq = kvh * p.qpk + (row - i0 * p.qpk);
         const float by = sum == 0.0f ? 1.0f : 1.0f / sum;
         unsigned char* to = p.out + ((t.start + i0) * p.ost + hq * p.osh) * 2;
@@ -1322,13 +1313,18 @@ Plan plan_attend(const squat_paged_store* s, squat_dtype dt, int n_seqs, int64_t
     if (max_kv < 1 || max_kv > room) max_kv = room;
     const int few = s->group / 8;                         // 16 columns, 128 / group of them a row
     a.nq = max_new * q_per_kv <= few ? 0 : max_new * q_per_kv <= 16 ? 1 : 2;
-    a.chunk = dt == SQUAT_BF16 && max_new * q_per_kv >= kChunkRows;
-    a.rows = a.chunk ? kChunkTile : a.nq == 0 ? few : 16 * a.nq;
-    a.tiles = n_new * q_per_kv / a.rows + n_seqs;
-    // tiles with work: what the hints allow
-    int64_t busy = n_seqs * ((max_new * q_per_kv + a.rows - 1) / a.rows);
-    busy = (busy < a.tiles ? busy : a.tiles) * s->n_kv_heads;
-    const int64_t steps = (max_kv + kStep - 1) / kStep, wanted = ((a.chunk ? 1 : a.nq > 0 ? kTargetRows : n_seqs < 4 ? kTargetOne : kTargetMany) * device_cu_count() + busy - 1) / busy;
+    // tiles, and those with work: what the hints allow
+    int64_t busy;
+    const auto tile = [&](int rows) {
+        a.rows = rows;
+        a.tiles = n_new * q_per_kv / rows + n_seqs;
+        busy = n_seqs * ((max_new * q_per_kv + rows - 1) / rows);
+        busy = (busy < a.tiles ? busy : a.tiles) * s->n_kv_heads;
+    };
+    tile(kChunkTile);
+    a.chunk = dt == SQUAT_BF16 && max_new * q_per_kv >= kChunkRows && busy >= device_cu_count() / 2;
+    if (!a.chunk) tile(a.nq == 0 ? few : 16 * a.nq);
+    const int64_t steps = (max_kv + kStep - 1) / kStep, wanted = a.chunk ? 1 : ((a.nq > 0 ? kTargetRows : n_seqs < 4 ? kTargetOne : kTargetMany) * device_cu_count() + busy - 1) / busy;
     int64_t span = (steps + wanted - 1) / wanted;
     span = span < kLeast ? kLeast : span;
     int64_t n = (steps + span - 1) / span;
@@ -1338,7 +1334,7 @@ Plan plan_attend(const squat_paged_store* s, squat_dtype dt, int n_seqs, int64_t
     n = a.rows > room_for ? 1 : n > room_for ? room_for : n;
     a.splits = n < 1 ? 1 : static_cast<int>(n);
     a.span = static_cast<int>((steps + a.splits - 1) / a.splits);
-    a.span = a.span < 1 ? 4 : (a.span + 3) & ~3;          // (whole steps of 128 tokens, for chunks)
+    a.span = a.span < 1 ? 1 : a.span;
     const size_t all = a.splits > 1 ? static_cast<size_t>(a.splits) * a.tiles * s->n_kv_heads * a.rows : 0;
     a.o_bytes = up256(all * kD * sizeof(float));
     a.ml_bytes = up256(all * sizeof(float2));
@@ -1474,8 +1470,7 @@ extern "C" int squat_paged_attention(const squat_paged_store* store, const void*
         case 4: launch_join<4>(q_dt, gx, s, p); break;
         case 8: launch_join<8>(q_dt, gx, s, p); break;
         case 16: launch_join<16>(q_dt, gx, s, p); break;
-        case 32: launch_join<32>(q_dt, gx, s, p); break;
-        default: launch_join<kChunkTile>(q_dt, gx, s, p); break;
+        default: launch_join<32>(q_dt, gx, s, p); break;
     }
     return check_launch();
 }

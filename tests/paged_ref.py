@@ -81,22 +81,25 @@ def attention(q, store, bits, table, lens, starts, out_scale, rounded_keys=False
             k = values(kc[ids, h].reshape(-1, kc.shape[-1]), km[ids, h].reshape(-1, *km.shape[-2:]), bits)[:length]
             v = values(vc[ids, h].reshape(-1, vc.shape[-1]), vm[ids, h].reshape(-1, *vm.shape[-2:]), bits)[:length]
             size = np.repeat(np.abs(km[ids, h].reshape(-1, *km.shape[-2:])[:length].astype(np.float64)) * [(bias + (1 << bits)), 1.0], D // km.shape[-2], -2).sum(-1)
-            for i in range(b - a):
-                seen = np.flatnonzero(there & (np.arange(length) <= length - (b - a) + i)) if length > 0 else np.zeros(0, np.int64)
-                if not len(seen):
+            for j in range(h * qpk, (h + 1) * qpk):
+                if length <= 0 or b == a:
                     continue
-                for j in range(h * qpk, (h + 1) * qpk):
-                    x = out_scale * (k[seen] @ q[a + i, j])
-                    m = x.max()
-                    p = np.exp(x - m)
-                    lse[a + i, j] = m + np.log(p.sum())
-                    p /= p.sum()
-                    out[a + i, j] = p @ v[seen]
-                    mass[a + i, j] = p @ np.abs(v[seen])
-                    # a logit: 128 products summed in fp32 from the bias on, then a handful of operations a group
-                    off[a + i, j] = abs(out_scale) * (size[seen] @ np.abs(q[a + i, j])).max() * 40 * 2.0 ** -24 + np.abs(x).max() * 2.0 ** -22
-                    if rounded_keys:
-                        off[a + i, j] += abs(out_scale) * (np.abs(k[seen]) @ np.abs(q[a + i, j])).max() * 2.0 ** -11
+                qj = q[a:b, j]
+                seen = there & (np.arange(length) <= length - (b - a) + np.arange(b - a)[:, None])
+                x = np.where(seen, out_scale * (qj @ k.T), -np.inf)
+                some = seen.any(1)
+                m = np.where(some, x.max(1), 0.0)
+                p = np.exp(x - m[:, None])
+                total = p.sum(1)
+                p = p / np.where(some, total, 1.0)[:, None]
+                with np.errstate(divide="ignore"):
+                    lse[a:b, j] = np.where(some, m + np.log(total), -np.inf)
+                out[a:b, j], mass[a:b, j] = p @ v, p @ np.abs(v)
+                # a logit: 128 products summed in fp32 from the bias on, then a handful of operations a group
+                worst = lambda y: np.where(seen, y, 0.0).max(1)       # noqa: E731
+                off[a:b, j] = abs(out_scale) * worst(np.abs(qj) @ size.T) * 40 * 2.0 ** -24 + worst(np.abs(x)) * 2.0 ** -22
+                if rounded_keys:
+                    off[a:b, j] += abs(out_scale) * worst(np.abs(qj) @ np.abs(k).T) * 2.0 ** -11
     return out, lse, mass, off
 
 

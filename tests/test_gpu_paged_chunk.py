@@ -1,4 +1,4 @@
-"""squat_paged_attention with many rows of bf16 queries, which meet dequantized keys and values: against the definition in 64 bits.  Keys are rounded
+"""squat_paged_attention with many rows of bf16 queries (2048 a sequence, and 128 tiles of 256 rows over the KV heads), which meet dequantized keys and values: against the definition in 64 bits.  Keys are rounded
 to fp16 there, so a logit's bound has 2^-11 of its products beside what test_gpu_paged_attention counts."""
 import numpy as np
 import pytest
@@ -21,25 +21,26 @@ def _run(seed, lens, new, heads, qpk, bits, group, page, scale=128 ** -0.5):
 
 @pytest.mark.parametrize("bits", [2, 4, 8])
 @pytest.mark.parametrize("group", [32, 64, 128])
-def test_chunk_in_parts(bits, group):
-    _run(bits + group, [700], [512], 1, 4, bits, group, 32)
+def test_chunk(bits, group):
+    _run(bits + group, [700], [512], 16, 4, bits, group, 32)
 
 
 @pytest.mark.parametrize("bits", [2, 4, 8])
-def test_chunk_in_one_part(bits):
-    _run(30 + bits, [200], [129], 1, 16, bits, 32, 16)
-    _run(40 + bits, [256], [128], 1, 16, bits, 128, 64, scale=-0.2)
+def test_steps_that_end_anywhere(bits):
+    _run(30 + bits, [200], [129], 16, 16, bits, 32, 16)
+    _run(40 + bits, [256], [128], 16, 16, bits, 128, 64, scale=-0.2)
+    _run(45 + bits, [385], [133], 16, 16, bits, 64, 16)
 
 
 def test_ragged_chunks():
     """Whole prompts, a chunk behind a long beginning, a decoded token and a sequence without tokens in one call; lengths that end inside a step."""
-    _run(50, [521, 1337, 90, 0, 31], [521, 77, 1, 0, 31], 1, 4, 4, 32, 64)
-    _run(51, [515, 1, 65], [515, 1, 40], 2, 4, 2, 64, 16)
+    _run(50, [521, 1337, 90, 0, 31], [521, 77, 1, 0, 31], 10, 4, 4, 32, 64)
+    _run(51, [515, 1, 65], [515, 1, 40], 12, 4, 2, 64, 16)
 
 
 def test_rows_that_see_nothing():
     """More new tokens than tokens."""
-    store, table, starts, q = _case(52, [100], [150], 1, 16, 4, 32, 16, "bf16")
+    store, table, starts, q = _case(52, [100], [150], 13, 16, 4, 32, 16, "bf16")
     lse = torch.full(q.shape[:2], 5.0, device="cuda")
     out = squat.paged_attention(q.cuda(), *P.to_device(store), 4, 32, _i32(table), _i32([100]), _i32(starts), 0.1, lse=lse)
     _close(out, lse, P.attention(q.double().numpy(), store, 4, table, [100], starts, 0.1, rounded_keys=True), "bf16")
@@ -48,7 +49,7 @@ def test_rows_that_see_nothing():
 
 @pytest.mark.parametrize("where", [0, 5, 12])
 def test_pages_that_do_not_exist(where):
-    store, table, starts, q = _case(53, [400], [128], 1, 16, 4, 32, 32, "bf16")
+    store, table, starts, q = _case(53, [400], [128], 16, 16, 4, 32, 32, "bf16")
     table[0, where] = -1
     lse = torch.full(q.shape[:2], 5.0, device="cuda")
     out = squat.paged_attention(q.cuda(), *P.to_device(store), 4, 32, _i32(table), _i32([400]), _i32(starts), 0.1, lse=lse)
@@ -60,7 +61,7 @@ def test_pages_that_do_not_exist(where):
 @pytest.mark.parametrize("length", [180, 600])
 def test_what_is_masked_does_not_show(what, which, length):
     new = 140
-    store, table, starts, q = _case(54, [length], [new], 2, 16, 4, 32, 16, "bf16")
+    store, table, starts, q = _case(54, [length], [new], 16, 16, 4, 32, 16, "bf16")
     dev = P.to_device(store)
     args = (4, 32, _i32(table), _i32([length]), _i32(starts), 0.1)
     clean = squat.paged_attention(q.cuda(), *dev, *args)
@@ -71,8 +72,8 @@ def test_what_is_masked_does_not_show(what, which, length):
     dev[1][table[0, length // 16], :, length % 16:] = what           # behind the end
     dev[3][table[0, length // 16], :, length % 16:] = what
     got = squat.paged_attention(q.cuda(), *dev, *args).cpu()
-    seen = torch.zeros(new, 32, dtype=torch.bool)
-    seen[at:, 16:] = True
+    seen = torch.zeros(new, 256, dtype=torch.bool)
+    seen[at:, 16:32] = True
     assert torch.equal(got[~seen], clean.cpu()[~seen])
     hit = got[seen]
     assert not (hit if which == "key" else hit[:, 64:96]).isfinite().any()
@@ -81,15 +82,15 @@ def test_what_is_masked_does_not_show(what, which, length):
 
 
 def test_strides_and_a_graph():
-    store, table, starts, q = _case(55, [300], [128], 1, 16, 4, 64, 32, "bf16")
+    store, table, starts, q = _case(55, [300], [128], 16, 16, 4, 64, 32, "bf16")
     dev = P.to_device(store)
     want = P.attention(q.double().numpy(), store, 4, table, [300], starts, 0.1, rounded_keys=True)
-    wide = torch.zeros(128, 20, 136, dtype=torch.bfloat16, device="cuda")
-    wide[:, 2:18, :128] = q.cuda()
-    big = torch.full((128, 3, 16, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    wide = torch.zeros(128, 260, 136, dtype=torch.bfloat16, device="cuda")
+    wide[:, 2:258, :128] = q.cuda()
+    big = torch.full((128, 3, 256, 128), 7.0, dtype=torch.bfloat16, device="cuda")
     tb, ln, st = _i32(table), _i32([300]), _i32(starts)
     ws = torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
-    run = lambda: squat.paged_attention(wide[:, 2:18, :128], *dev, 4, 64, tb, ln, st, 0.1, out=big[:, 1], ws=ws)        # noqa: E731
+    run = lambda: squat.paged_attention(wide[:, 2:258, :128], *dev, 4, 64, tb, ln, st, 0.1, out=big[:, 1], ws=ws)        # noqa: E731
     run()
     _close(big[:, 1], None, want, "bf16")
     assert (big[:, 0] == 7).all() and (big[:, 2] == 7).all()
