@@ -125,32 +125,47 @@ __device__ __forceinline__ uint32_t byte_perm(uint32_t a, uint32_t b, uint32_t s
 __device__ __forceinline__ float half_lo(uint32_t u) { return static_cast<float>(as_half2(u)[0]); }
 __device__ __forceinline__ float half_hi(uint32_t u) { return static_cast<float>(as_half2(u)[1]); }
 
-// What is added to a code when its bits are put into an fp16 mantissa.
+// Codes become fp16 by placing their bits in the mantissa of a power of two, the bias, whose size goes by where in a half word they come to lie (from
+// bit b up: 2^(10 - b)).  What is masked out is merged with it in one operation, and codes stay where two or three of them fit the mantissa:
+// ten operations for the eight pairs of a word of 2 bits, six for four of 4 bits (a shift for each but one: 15 and 7).
 template <int BITS>
-struct Bias {
-    static constexpr float value = BITS == 2 ? 16.0f : BITS == 4 ? 64.0f : 1024.0f;
-    static constexpr uint32_t bits = BITS == 2 ? 0x4C004C00u : BITS == 4 ? 0x54005400u : 0x64006400u;
-};
-
-__device__ __forceinline__ uint32_t shifted(uint32_t x, int left) { return left >= 0 ? x << left : x >> -left; }
-
-// The constants of the unpacking, one and the other in registers, so that masking and placing is one operation.
 struct Places {
-    uint32_t mask, bias;
+    static constexpr int N = BITS == 2 ? 3 : BITS == 4 ? 2 : 1;
+    uint32_t mask[N], bias[N];
+    static constexpr int bit(int k) { return BITS == 2 ? 4 + 2 * k : BITS == 4 ? 2 + 4 * k : 0; }
+    __device__ __forceinline__ Places() {                 // one and the other in registers
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            mask[k] = (((1u << BITS) - 1u) << bit(k)) * 0x10001u;
+            bias[k] = static_cast<uint32_t>(0x6400 - 0x400 * bit(k)) * 0x10001u;
+            asm("" : "+s"(mask[k]));
+            asm("" : "+v"(bias[k]));
+        }
+    }
 };
+
+// Which place code i of a half word has, and the bias it gets there.
 template <int BITS>
-__device__ __forceinline__ Places places() {
-    constexpr int at = BITS == 2 ? 6 : 4;
-    Places c{(((1u << BITS) - 1u) << at) * 0x10001u, Bias<BITS>::bits};
-    asm("" : "+s"(c.mask));
-    asm("" : "+v"(c.bias));
-    return c;
+__device__ __forceinline__ constexpr int place_of(int i) {
+    return BITS == 2 ? (i < 2 ? i : i < 5 ? i - 2 : i - 5) : BITS == 4 ? (i & 1) : 0;
+}
+template <int BITS>
+__device__ __forceinline__ constexpr float bias_of(int i) {
+    return static_cast<float>(1 << (10 - Places<BITS>::bit(place_of<BITS>(i))));
+}
+template <int BITS>
+__device__ __forceinline__ half2v bias_pair(int i) {
+    return half2v{static_cast<_Float16>(bias_of<BITS>(i)), static_cast<_Float16>(bias_of<BITS>(i))};
 }
 
-// Two codes of `x` (halves), at bit b of each half (2 and 4 bits), as bias + code.
+// Code i of both halves of x (2 and 4 bits), as bias + code.
 template <int BITS>
-__device__ __forceinline__ uint32_t code_pair(uint32_t x, int b, const Places& c) {
-    return (shifted(x, (BITS == 2 ? 6 : 4) - b) & c.mask) | c.bias;
+__device__ __forceinline__ uint32_t code_pair(uint32_t x, int i, const Places<BITS>& c) {
+    const int k = place_of<BITS>(i);
+    uint32_t y;
+    if constexpr (BITS == 2) y = i < 2 ? x << 4 : i < 5 ? x : x >> 6;
+    else y = i < 2 ? x << 2 : x >> 6;
+    return (y & c.mask[k]) | c.bias[k];
 }
 
 // Where in a row of a step kept in LDS (see Stage) its 16-byte piece `piece` is.
@@ -169,7 +184,8 @@ struct KeyWords<2> {
     __device__ __forceinline__ void load_turned(const unsigned char* p, int m, int h) { w = *reinterpret_cast<const u32x2*>(p + 32 * m + 8 * h); }
     static __device__ __forceinline__ constexpr int channel(int s, int e) { return 16 * (s >> 1) + 4 * (s & 1) + (e >> 1) + 8 * (e & 1); }
     __device__ __forceinline__ void load(const unsigned char* p) { w = *reinterpret_cast<const u32x2*>(p); }
-    __device__ __forceinline__ uint32_t pair(int s, int r, const Places& c) const { return code_pair<2>(w[s >> 1], 8 * (s & 1) + 2 * r, c); }
+    static __device__ __forceinline__ constexpr int code(int s, int r) { return 4 * (s & 1) + r; }       // of the pair: see bias_of
+    __device__ __forceinline__ uint32_t pair(int s, int r, const Places<2>& c) const { return code_pair<2>(w[s >> 1], code(s, r), c); }
 };
 template <>
 struct KeyWords<4> {
@@ -179,7 +195,8 @@ struct KeyWords<4> {
     }
     static __device__ __forceinline__ constexpr int channel(int s, int e) { return 8 * s + (e >> 1) + 4 * (e & 1); }
     __device__ __forceinline__ void load(const unsigned char* p) { w = *reinterpret_cast<const u32x4*>(p); }
-    __device__ __forceinline__ uint32_t pair(int s, int r, const Places& c) const { return code_pair<4>(w[s], 4 * r, c); }
+    static __device__ __forceinline__ constexpr int code(int, int r) { return r; }
+    __device__ __forceinline__ uint32_t pair(int s, int r, const Places<4>& c) const { return code_pair<4>(w[s], r, c); }
 };
 template <>
 struct KeyWords<8> {
@@ -193,8 +210,9 @@ struct KeyWords<8> {
         w[0] = *reinterpret_cast<const u32x4*>(p);
         w[1] = *reinterpret_cast<const u32x4*>(p + 16);
     }
-    __device__ __forceinline__ uint32_t pair(int s, int r, const Places& c) const {
-        return byte_perm(c.bias, w[s >> 1][2 * (s & 1) + (r >> 1)], (r & 1) ? 0x05030502u : 0x05010500u);
+    static __device__ __forceinline__ constexpr int code(int, int) { return 0; }
+    __device__ __forceinline__ uint32_t pair(int s, int r, const Places<8>& c) const {
+        return byte_perm(c.bias[0], w[s >> 1][2 * (s & 1) + (r >> 1)], (r & 1) ? 0x05030502u : 0x05010500u);
     }
 };
 
@@ -211,14 +229,15 @@ struct ValueWord {
 
 // Channel j of two tokens, as bias + code.
 template <int BITS>
-__device__ __forceinline__ uint32_t value_pair(const ValueWord<BITS>& a, const ValueWord<BITS>& b, int j, const Places& c) {
+__device__ __forceinline__ uint32_t value_pair(const ValueWord<BITS>& a, const ValueWord<BITS>& b, int j, const Places<BITS>& c) {
     if constexpr (BITS == 2) {
-        return code_pair<2>(static_cast<uint32_t>(a.w) | (static_cast<uint32_t>(b.w) << 16), 2 * j, c);
+        return code_pair<2>(static_cast<uint32_t>(a.w) | (static_cast<uint32_t>(b.w) << 16), j, c);
     } else if constexpr (BITS == 4) {
-        return code_pair<4>(byte_perm(b.w, a.w, j < 4 ? 0x05040100u : 0x07060302u), 4 * (j & 3), c);
+        return code_pair<4>(byte_perm(b.w, a.w, j < 4 ? 0x05040100u : 0x07060302u), j & 3, c);
     } else {
-        const uint32_t k = static_cast<uint32_t>(j & 3);
-        return byte_perm(b.w[j >> 2], a.w[j >> 2], 0x0C000C00u | k | ((k + 4u) << 16)) | c.bias;
+        // (two channels of both tokens side by side, then one of them into the halves)
+        const uint32_t two = byte_perm(b.w[j >> 2], a.w[j >> 2], (j & 2) ? 0x07030602u : 0x05010400u);
+        return byte_perm(c.bias[0], two, (j & 1) ? 0x05030502u : 0x05010500u);
     }
 }
 
@@ -271,10 +290,10 @@ __device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) {
 }
 
 // A lane's 32 channels of a query as operands, in KeyWords' order, times a power of two that brings the row's largest element into [1/2, 1);
-// `scale`: what turns the row's products into powers of two; `sum`: the operands' sum.  `keep`: whether they count (else 0); rows that are
+// `scale`: what turns the row's products into powers of two; `sum`: the operands' sum, `biased`: with the biases of the codes they meet.  `keep`: whether they count (else 0); rows that are
 // not live are 0 too.  (Elements below 2^-14 of the largest lose bits to fp16's range: 2^-25 of it at most.)
 template <int BITS, int QDT>
-__device__ __forceinline__ void load_query(const AttendParams& p, const unsigned char* src, bool live, bool keep, half8 (&qf)[4], float& scale, float& sum) {
+__device__ __forceinline__ void load_query(const AttendParams& p, const unsigned char* src, bool live, bool keep, half8 (&qf)[4], float& scale, float& sum, float& biased) {
     u32x4 raw[4];
 #pragma unroll
     for (int s = 0; s < 4; ++s) raw[s] = *reinterpret_cast<const u32x4*>(src + 16 * s);
@@ -293,7 +312,7 @@ __device__ __forceinline__ void load_query(const AttendParams& p, const unsigned
     e2 = max(-100, min(100, e2));
     const float factor = ldexpf(live && keep ? (p.scale < 0.0f ? -1.0f : 1.0f) : 0.0f, -e2);
     scale = fmaxf(ldexpf(fabsf(p.scale), e2), 1e-30f);
-    sum = 0.0f;
+    sum = biased = 0.0f;
     if (!(live && keep)) {                                // (not by a product: what another group holds need not be finite)
 #pragma unroll
         for (int s = 0; s < 4; ++s) raw[s] = u32x4{0u, 0u, 0u, 0u};
@@ -308,8 +327,11 @@ __device__ __forceinline__ void load_query(const AttendParams& p, const unsigned
             qf[s][e] = static_cast<_Float16>(x * factor);
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            sum = __builtin_amdgcn_fdot2(half2v{qf[s][2 * e], qf[s][2 * e + 1]}, half2v{static_cast<_Float16>(1.0f), static_cast<_Float16>(1.0f)}, sum, false);
+        for (int e = 0; e < 4; ++e) {
+            const half2v two = {qf[s][2 * e], qf[s][2 * e + 1]};
+            sum = __builtin_amdgcn_fdot2(two, half2v{static_cast<_Float16>(1.0f), static_cast<_Float16>(1.0f)}, sum, false);
+            biased = __builtin_amdgcn_fdot2(two, bias_pair<BITS>(KeyWords<BITS>::code(s, e)), biased, false);
+        }
     }
 }
 
@@ -427,8 +449,8 @@ __global__ void __launch_bounds__(256) attend_kernel(const AttendParams p) {
         const int r = live ? row : t.rows - 1;
         const int i = r / p.qpk, hq = kvh * p.qpk + (r - i * p.qpk);
         seen[n] = live ? t.pos0 + i : -1;
-        float sum;
-        load_query<BITS, QDT>(p, p.q + ((t.start + i) * p.qst + hq * p.qsh + 32 * h) * 2, live, true, qf[n], scale[n], sum);
+        float sum, biased;
+        load_query<BITS, QDT>(p, p.q + ((t.start + i) * p.qst + hq * p.qsh + 32 * h) * 2, live, true, qf[n], scale[n], sum, biased);
         slack[n] = kSlack / scale[n];
 #pragma unroll
         for (int e = 0; e < 8; ++e) qz[n][e] = static_cast<_Float16>(0.0f);
@@ -436,8 +458,7 @@ __global__ void __launch_bounds__(256) attend_kernel(const AttendParams p) {
         qz[n][1] = static_cast<_Float16>(sum - static_cast<float>(qz[n][0]));
     }
     const int least_seen = t.pos0 + t.row0 / p.qpk;       // every live row sees this token and all before it
-    const Places places_ = places<BITS>();
-    const half2v bias = {static_cast<_Float16>(Bias<BITS>::value), static_cast<_Float16>(Bias<BITS>::value)};
+    const Places<BITS> places_;
 
     f32x4 o[NQ][8], total[NQ];                            // O^T: channels 8 (4 h + i) + j, column m; the weights' sum
     float top[NQ];
@@ -481,7 +502,7 @@ __global__ void __launch_bounds__(256) attend_kernel(const AttendParams p) {
                 u32x4 hi, lo;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const half2v c = as_half2(kw[u].pair(s, r, places_)) - bias;
+                    const half2v c = as_half2(kw[u].pair(s, r, places_)) - bias_pair<BITS>(KeyWords<BITS>::code(s, r));
                     const half2v y = c * ks;              // code * scale without its rounding: a high and a low part
                     hi[r] = __builtin_bit_cast(uint32_t, y);
                     lo[r] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(c, ks, -y));
@@ -580,7 +601,7 @@ __global__ void __launch_bounds__(256) attend_kernel(const AttendParams p) {
             u32x4 raw;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const half2v c = as_half2(value_pair<BITS>(vw[e >> 1][2 * (e & 1)], vw[e >> 1][2 * (e & 1) + 1], j, places_)) - bias;
+                const half2v c = as_half2(value_pair<BITS>(vw[e >> 1][2 * (e & 1)], vw[e >> 1][2 * (e & 1) + 1], j, places_)) - bias_pair<BITS>(BITS == 4 ? j & 3 : j);
                 raw[e] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(c, vs[e], vz[e]));
             }
             const half8 vf = __builtin_bit_cast(half8, raw);
@@ -731,14 +752,16 @@ __global__ void __launch_bounds__(256) attend_few_kernel(const AttendParams p) {
     const int qi = (live ? row : t.rows - 1) / p.qpk, hq = kvh * p.qpk + (live ? row : t.rows - 1) - qi * p.qpk;
     const int seen = live ? t.pos0 + qi : -1;             // the last token that the row sees
     half8 qf[4];
-    float scale, group_sum;
-    load_query<BITS, QDT>(p, p.q + ((t.start + qi) * p.qst + hq * p.qsh + 32 * h) * 2, live, (h * NG) >> 2 == g, qf, scale, group_sum);
+    float scale, group_sum, biased;
+    load_query<BITS, QDT>(p, p.q + ((t.start + qi) * p.qst + hq * p.qsh + 32 * h) * 2, live, (h * NG) >> 2 == g, qf, scale, group_sum, biased);
     group_sum += __shfl_xor(group_sum, 16, 64);
     group_sum += __shfl_xor(group_sum, 32, 64);
-    const float slack = kSlack / scale, neg = -Bias<BITS>::value * group_sum;
-    const f32x4 start = {neg, neg, neg, neg};
+    biased += __shfl_xor(biased, 16, 64);
+    biased += __shfl_xor(biased, 32, 64);
+    const float slack = kSlack / scale;
+    const f32x4 start = {-biased, -biased, -biased, -biased};
     const int least_seen = t.pos0 + t.row0 / p.qpk;       // every live row sees this token and all before it
-    const Places places_ = places<BITS>();
+    const Places<BITS> places_;
     const half2v zero2 = {static_cast<_Float16>(0.0f), static_cast<_Float16>(0.0f)};
 
     f32x4 o[8], weight = {0.0f, 0.0f, 0.0f, 0.0f};        // O^T: channels 8 (4 h + i) + j; the sum of p scale
@@ -879,15 +902,18 @@ __global__ void __launch_bounds__(256) attend_few_kernel(const AttendParams p) {
         scales += __shfl_xor(scales, 32, 64);
         zeros = fmaf(MIDDLE, scales, zeros);
     }
-    const float back = ldexpf(1.0f, shift), add = fmaf(-(Bias<BITS>::value + MIDDLE), weight[0], zeros);
+    const float back = ldexpf(1.0f, shift);
+    float add[8];                                         // to channel j of the lane's eight
+#pragma unroll
+    for (int j = 0; j < 8; ++j) add[j] = fmaf(-(bias_of<BITS>(BITS == 4 ? j & 3 : j) + MIDDLE), weight[0], zeros);
     __syncthreads();                                      // (nobody reads steps any more)
     if (h == 0 && g == 0) stats[wave][rr] = float2{top > -INFINITY ? top * scale : -INFINITY, total * back};
     if ((h * NG) >> 2 == g) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             float* to = &sums[wave][rr][32 * h + 8 * i];
-            *reinterpret_cast<f32x4*>(to) = f32x4{o[0][i] + add, o[1][i] + add, o[2][i] + add, o[3][i] + add} * back;
-            *reinterpret_cast<f32x4*>(to + 4) = f32x4{o[4][i] + add, o[5][i] + add, o[6][i] + add, o[7][i] + add} * back;
+            *reinterpret_cast<f32x4*>(to) = f32x4{o[0][i] + add[0], o[1][i] + add[1], o[2][i] + add[2], o[3][i] + add[3]} * back;
+            *reinterpret_cast<f32x4*>(to + 4) = f32x4{o[4][i] + add[4], o[5][i] + add[5], o[6][i] + add[6], o[7][i] + add[7]} * back;
         }
     }
     __syncthreads();
@@ -930,8 +956,7 @@ __global__ void __launch_bounds__(64 * kChunkWaves, 2) attend_chunk_kernel(const
     const int last = (t.steps + 3) / 4;                   // steps of 128 tokens
     const Walk walk(p, t, kvh);
     const int least_seen = t.pos0 + t.row0 / p.qpk;       // every row of the tile sees this token and all before it
-    const Places places_ = places<BITS>();
-    const half2v bias = {static_cast<_Float16>(Bias<BITS>::value), static_cast<_Float16>(Bias<BITS>::value)};
+    const Places<BITS> places_;
 
     // What this wavefront dequantizes: quarter wave & 3 of a step.
     const bool of_keys = wave >= 4;                       // uniform
@@ -995,10 +1020,11 @@ __global__ void __launch_bounds__(64 * kChunkWaves, 2) attend_chunk_kernel(const
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     uint32_t x;
-                    if constexpr (BITS == 2) x = code_pair<2>(kw[k >> 1], 8 * (k & 1) + 2 * r, places_);
-                    else if constexpr (BITS == 4) x = code_pair<4>(kw[k], 4 * r, places_);
-                    else x = byte_perm(places_.bias, kw[2 * k + (r >> 1)], (r & 1) ? 0x05030502u : 0x05010500u);
-                    y[r] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(as_half2(x) - bias, ks[g], kz[g]));
+                    const int i = BITS == 2 ? 4 * (k & 1) + r : r;
+                    if constexpr (BITS == 2) x = code_pair<2>(kw[k >> 1], i, places_);
+                    else if constexpr (BITS == 4) x = code_pair<4>(kw[k], i, places_);
+                    else x = byte_perm(places_.bias[0], kw[2 * k + (r >> 1)], (r & 1) ? 0x05030502u : 0x05010500u);
+                    y[r] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(as_half2(x) - bias_pair<BITS>(i), ks[g], kz[g]));
                 }
                 *reinterpret_cast<u32x4*>(to + 16 * k) = y;
             }
@@ -1032,7 +1058,7 @@ __global__ void __launch_bounds__(64 * kChunkWaves, 2) attend_chunk_kernel(const
                 u32x4 y;
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    y[e] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(as_half2(value_pair<BITS>(vw[e >> 1][2 * (e & 1)], vw[e >> 1][2 * (e & 1) + 1], j, places_)) - bias,
+                    y[e] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(as_half2(value_pair<BITS>(vw[e >> 1][2 * (e & 1)], vw[e >> 1][2 * (e & 1) + 1], j, places_)) - bias_pair<BITS>(BITS == 4 ? j & 3 : j),
                                                                                   vs[e], vz[e]));
                 *reinterpret_cast<u32x4*>(values[place][quarter][j] + 16 * lane) = y;
             }
