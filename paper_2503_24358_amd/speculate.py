@@ -1,0 +1,154 @@
+"""Speculative decoding from a paged, quantized cache: what a serving loop does with squat.PagedStore and squat.verify_drafts.
+
+One attention layer with random weights stands in for a model (`Model`); prompts of different lengths arrive in chunks, then every
+step drafts a few tokens per sequence, writes the keys and values of the last token and its drafts to the sequence's pages, lets
+them attend to everything the sequence has, and keeps as many drafts as the target's probabilities allow.  Nothing in the loop
+waits for the device: lengths, slots and tokens stay there.
+
+    python -m paper_2503_24358_amd.speculate
+"""
+from __future__ import annotations
+
+import math
+import time
+
+import torch
+
+from paper_2503_24358_amd import squat
+
+D = 128
+
+
+class Model:
+    """An embedding, one grouped-query attention layer and a vocabulary, all random; a bigram table made from them drafts."""
+
+    def __init__(self, vocab: int = 4096, heads: int = 2, q_per_kv: int = 4, width: int = 512, seed: int = 0, device="cuda"):
+        g = torch.Generator(device=device).manual_seed(seed)
+        rand = lambda *shape: torch.randn(shape, generator=g, device=device) / math.sqrt(shape[0])      # noqa: E731
+        self.vocab, self.heads, self.q_per_kv = vocab, heads, q_per_kv
+        self.embed = torch.randn((vocab, width), generator=g, device=device)
+        self.wq, self.wk, self.wv = rand(width, heads * q_per_kv * D), rand(width, heads * D), rand(width, heads * D)
+        self.wo = rand(heads * q_per_kv * D, width)
+        self.head = rand(width, vocab) * 6.0
+
+    def projections(self, tokens: torch.Tensor):
+        """Queries, keys and values of tokens [n], bf16 [n, heads, 128]."""
+        x = self.embed[tokens]
+        return [(x @ w).view(len(tokens), -1, D).bfloat16() for w in (self.wq, self.wk, self.wv)]
+
+    def logits(self, tokens: torch.Tensor, attended: torch.Tensor) -> torch.Tensor:
+        return (self.embed[tokens] + attended.float().reshape(len(tokens), -1) @ self.wo) @ self.head
+
+    def bigram(self, tokens: torch.Tensor) -> torch.Tensor:
+        """Draft logits: the model without its attention."""
+        return self.embed[tokens] @ self.head
+
+
+class Engine:
+    """A batch of sequences of different lengths over one paged store."""
+
+    def __init__(self, model: Model, prompts, new_tokens: int, drafts: int, *, bits: int = 4, group: int = 32, page: int = 32,
+                 subspace: int = 0, greedy: bool = False, seed: int = 0):
+        self.model, self.drafts, self.page, self.greedy = model, drafts, page, greedy
+        dev = model.embed.device
+        self.gen = torch.Generator(device=dev).manual_seed(seed)
+        n = len(prompts)
+        # pages for the longest that a sequence can become, dealt out in turn (a sequence's pages lie anywhere)
+        per_seq = [-(-(len(p) + new_tokens + drafts + 1) // page) for p in prompts]
+        self.store = squat.PagedStore(sum(per_seq), model.heads, page, bits, group, device=dev)
+        table = torch.zeros((n, max(per_seq)), dtype=torch.int32)
+        order = iter(torch.randperm(sum(per_seq)).tolist())
+        for i, count in enumerate(per_seq):
+            table[i, :count] = torch.tensor([next(order) for _ in range(count)], dtype=torch.int32)
+        self.table = table.to(dev)
+        self.max_kv = max(per_seq) * page
+        self.kv_len = torch.zeros(n, dtype=torch.int32, device=dev)
+        self.update = None
+        if subspace:
+            # the subspace of the first prompt's queries, and the update matrix of its heads for all sequences
+            q = model.projections(prompts[0].to(dev))[0].transpose(0, 1).contiguous()
+            qhat, _, _ = squat.build_subspace(q, model.q_per_kv, subspace)
+            self.update = squat.prepare(qhat, 1e-3, 32)
+        self.last = torch.stack([p[-1] for p in prompts]).to(dev)
+        self._prefill([p[:-1].to(dev) for p in prompts])
+
+    def _slots(self, seq: torch.Tensor, position: torch.Tensor) -> torch.Tensor:
+        return self.table[seq, position // self.page].long() * self.page + position % self.page
+
+    def _attend(self, tokens, starts, seq, position, most):
+        """Writes the tokens' keys and values and returns what their queries gather; kv_len counts them already."""
+        q, k, v = self.model.projections(tokens)
+        self.store.write(k, v, self._slots(seq, position), update=self.update)
+        return self.store.attention(q, self.table, self.kv_len, starts, 1.0 / math.sqrt(D), max_new=most, max_kv=self.max_kv)
+
+    def _prefill(self, prompts, chunk: int = 256):
+        dev = self.table.device
+        done = [0] * len(prompts)
+        while any(d < len(p) for d, p in zip(done, prompts)):
+            take = [min(chunk, len(p) - d) for d, p in zip(done, prompts)]
+            tokens = torch.cat([p[d:d + t] for p, d, t in zip(prompts, done, take)])
+            seq = torch.cat([torch.full((t,), i, device=dev) for i, t in enumerate(take)])
+            position = torch.cat([torch.arange(d, d + t, device=dev) for d, t in zip(done, take)])
+            starts = torch.tensor([0] + take, dtype=torch.int32).cumsum(0, dtype=torch.int32).to(dev)
+            self.kv_len += torch.tensor(take, dtype=torch.int32, device=dev)
+            self._attend(tokens, starts, seq, position, max(take))
+            done = [d + t for d, t in zip(done, take)]
+
+    def _probabilities(self, logits):
+        if self.greedy:
+            return torch.zeros_like(logits).scatter_(-1, logits.argmax(-1, keepdim=True), 1.0)
+        return torch.softmax(logits, -1)
+
+    def step(self):
+        """One pass of the target over the last token and `drafts` drafted ones; returns (accepted [n], tokens [n, drafts + 1])."""
+        n, k, dev = len(self.last), self.drafts, self.table.device
+        # drafts, one after the other, from the bigram table
+        tokens, probs = [self.last], []
+        for _ in range(k):
+            p = torch.softmax(self.model.bigram(tokens[-1]), -1)
+            probs.append(p)
+            tokens.append(torch.multinomial(p, 1, generator=self.gen)[:, 0])
+        tokens = torch.stack(tokens, 1)                                     # [n, k + 1]: the last token and its drafts
+        before = self.kv_len.long()
+        self.kv_len += k + 1
+        seq = torch.arange(n, device=dev).repeat_interleave(k + 1)
+        position = (before.unsqueeze(1) + torch.arange(k + 1, device=dev)).reshape(-1)
+        starts = torch.arange(n + 1, dtype=torch.int32, device=dev) * (k + 1)
+        attended = self._attend(tokens.reshape(-1), starts, seq, position, k + 1)
+        target = self._probabilities(self.model.logits(tokens.reshape(-1), attended)).view(n, k + 1, -1)
+        accepted, out = squat.verify_drafts(tokens[:, 1:].contiguous(), target, torch.stack(probs, 1) if k else None,
+                                            torch.rand((n, k), generator=self.gen, device=dev), torch.rand((n,), generator=self.gen, device=dev))
+        # the last token and the accepted drafts stay; what lies behind them is written over by the next step
+        self.kv_len = (before + accepted + 1).to(torch.int32)
+        self.last = out.gather(1, accepted.long().unsqueeze(1))[:, 0]
+        return accepted, out
+
+
+def generate(engine: Engine, new_tokens: int):
+    """At least `new_tokens` tokens of every sequence: a list of lists, and the number of steps."""
+    texts, steps = [[] for _ in range(len(engine.last))], 0
+    room = engine.kv_len + new_tokens
+    while min(len(t) for t in texts) < new_tokens:
+        accepted, out = engine.step()
+        for t, a, row in zip(texts, accepted.tolist(), out.tolist()):
+            t.extend(row[:a + 1])
+        # a sequence that is ahead of the others and has what was asked for starts over behind its own beginning
+        engine.kv_len = torch.minimum(engine.kv_len, room)
+        steps += 1
+    return [t[:new_tokens] for t in texts], steps
+
+
+def main():
+    model = Model()
+    g = torch.Generator().manual_seed(1)
+    prompts = [torch.randint(0, model.vocab, (length,), generator=g) for length in (700, 33, 1200, 1, 256)]
+    for drafts in (0, 4):
+        engine = Engine(model, prompts, 64, drafts, subspace=16)
+        torch.cuda.synchronize()
+        began = time.perf_counter()
+        texts, steps = generate(engine, 64)
+        print("%d drafts a step: %d sequences, 64 tokens each, %d steps, %.1f ms" % (drafts, len(texts), steps, (time.perf_counter() - began) * 1e3))
+
+
+if __name__ == "__main__":
+    main()
