@@ -967,7 +967,8 @@ __global__ void __launch_bounds__(64 * kChunkWaves, 2) attend_chunk_kernel(const
     uint32_t vm[2][4];
     int limit[2];
     const int key_row = lane >> 1, key_half = lane & 1;
-    Pages ahead = walk.pages(quarter);
+    Pages ahead{};
+    if (last > 0) ahead = walk.pages(quarter);            // (without tokens there need not be a list)
     const auto load = [&](int step) {                     // of 128 tokens; `ahead` are its pages, and then the next one's
         const Place a = walk.place(4 * step + quarter, ahead);
         ahead = walk.pages(4 * step + 4 + quarter);

@@ -47,6 +47,18 @@ def test_rows_that_see_nothing():
     assert (out[:50] == 0).all() and torch.isneginf(lse[:50]).all()
 
 
+@pytest.mark.parametrize("new, heads, qpk", [(150, 13, 16), (2, 3, 2), (9, 3, 4)])
+def test_lists_of_no_pages(new, heads, qpk):
+    """The lists may be nowhere where no sequence has room for a token (this form, one row a step, and several)."""
+    store, _, starts, q = _case(56, [0], [new], heads, qpk, 4, 32, 16, "bf16")
+    lse = torch.full(q.shape[:2], 5.0, device="cuda")
+    out = torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda")
+    for length in (0, 700):
+        squat.paged_attention(q.cuda(), *P.to_device(store), 4, 32, torch.empty((1, 0), dtype=torch.int32, device="cuda"), _i32([length]), _i32(starts),
+                              0.1, out=out, lse=lse)
+        assert (out == 0).all() and torch.isneginf(lse).all()
+
+
 @pytest.mark.parametrize("where", [0, 5, 12])
 def test_pages_that_do_not_exist(where):
     store, table, starts, q = _case(53, [400], [128], 16, 16, 4, 32, 32, "bf16")
