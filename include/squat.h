@@ -681,8 +681,8 @@ int squat_paged_read(const squat_paged_store* store, const int64_t* slots, int64
  *     p = softmax_{t <= P}(out_scale * q . k_t),    lse = log sum_t exp(...)
  * with k_t, v_t as squat_paged_read gives them (fp32).  A token that sees nothing
  * (P < 0) gives zeros and lse = -infinity.  A token whose scale or zero-point is
- * not finite gives NaN to what sees it (a key's to the whole row, a value's to
- * its group's channels), and to nothing else.
+ * not finite gives NaN or infinity to what sees it (a key's to the whole row, a
+ * value's to its group's channels), and to nothing else.
  *
  *   q        [n_new, n_kv_heads*q_per_kv, d] dtype q_dt (fp16 or bf16), element
  *            (t,hq,c) at q[t*q_stride_token + hq*q_stride_head + c]; base 16-byte
@@ -702,9 +702,12 @@ int squat_paged_read(const squat_paged_store* store, const int64_t* slots, int64
  *   lse      [n_new, n_kv_heads*q_per_kv] float, dense, or NULL.
  *   ws       scratch of squat_paged_attention_workspace(...) bytes for the same
  *            arguments, 256-byte aligned (NULL where that is 0).
- * Products of queries and codes or keys are taken in fp16 with sums in fp32
- * (bf16 queries are brought into fp16's range by a power of two per row first);
- * statistics of the softmax and the result are held in fp32 until the end.
+ * Both products are taken in fp16 with sums in fp32 (queries are brought into
+ * fp16's range by a power of two per row first); statistics of the softmax and the
+ * result are held in fp32 until the end.  The softmax's weights are rounded to fp16
+ * (2^-11 of each), from 17 - 128 / group rows per KV head and sequence on the
+ * values too.  Keys enter exactly, but where a sequence can have 2048 rows per KV
+ * head or more of bf16 queries: there they may be rounded to fp16 as well.
  * ------------------------------------------------------------------------- */
 size_t squat_paged_attention_workspace(const squat_paged_store* store, int n_seqs, int64_t n_new, int q_per_kv,
                                        int pages_per_seq, int64_t max_new, int64_t max_kv);

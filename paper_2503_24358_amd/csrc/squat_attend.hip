@@ -1,18 +1,23 @@
 // squat_paged_attention: softmax(scale q k^T) v over a store of pages, straight from the packed codes.
 //
-// Rows are (new token, query head of a KV head) pairs of one sequence, in tiles of 16 or 32; a workgroup meets one tile and one KV
-// head with a part of the sequence, its four wavefronts taking 32-token steps in turn.  Per step a wavefront computes
-// S^T = K Q^T and O^T += V^T P^T with 16x16x32 fp16 matrix instructions: in both a lane's column is a query row, so that the
-// softmax's maximum and sum stay in the lane, and the logits of a lane (tokens 4 h + i of the step's halves, h = lane / 16) are
-// where the second product wants its operand: nothing is exchanged between lanes and nothing goes through LDS.
+// Rows are (new token, query head of a KV head) pairs of one sequence, in tiles; a workgroup meets one tile and one KV head with a part of the
+// sequence, in steps of tokens.  Per step a wavefront computes S^T = K Q^T and O^T += V^T P^T with 16x16x32 fp16 matrix instructions: in
+// both a lane's column is a query row, so that the softmax's maximum and sum stay in the lane, and the logits of a lane (tokens 4 h + i of
+// the step's halves, h = lane / 16) are where the second product wants its operand: nothing is exchanged between lanes.  The order of channels and
+// tokens within the products is free, so that neither needs a transpose.  Three forms, by the rows a tile can have:
+//   - a few rows (a decoded token's query heads): codes enter the products as integers, the 16 columns hold the groups.  Bound: the store's bytes
+//     for 8 bits, the vector instructions of the unpacking for 2 (attend_few_kernel).
+//   - 16 or 32 rows (drafted tokens, short chunks): keys as a high and a low fp16 part, which is exact for every code, values dequantized to
+//     fp16 (attend_kernel).  Bound: the unpacking, and for short calls the chain of a part: first loads, 32 rows of sums, putting them together.
+//   - many rows of bf16 (prefill): keys and values dequantized once, through LDS, for 256 rows (attend_chunk_kernel).  Bound: the products.
 //
-// Codes become fp16 by placing their bits in the mantissa of a power of two (bias + code, one or two operations per pair); less the bias,
-// they are dequantized by one fused multiply-add, one rounding (2^-11), in the lane that holds them: a quarter of a key's channels with
-// one scale, or 8 channels of 8 tokens of the values, which the second product needs as 8 operands of 8 tokens, one per channel.
-// The order of channels and tokens within the products is free, so that neither needs a transpose.
+// Codes become fp16 by placing their bits in the mantissa of a power of two (bias + code, one or two operations per pair).
 //
 // The running maximum m of a row is raised only when a logit passes it by more than 2^kSlack (the rows' sums are rescaled then, for
 // all of them): p = 2^(x - m + kLift), at most 2^15, and small weights keep their bits down to 2^-(24 + kLift) of the largest.
+//
+// us on one MI355X, launch included (bf16, 8 KV heads): a decoded token of 64 sequences to 8192 tokens, 2 bits, 71.7 (3.2 TB/s of store); one of
+// 131072, 4 bits, 38 (4.0 TB/s); 6 tokens of each of 16 to 4100, 8 bits, 33 (2.7 TB/s); 2048 over 16384, 4 bits, 557 (924 TFLOP/s).
 #include <type_traits>
 
 #include "squat_paged.h"
@@ -632,7 +637,8 @@ __global__ void __launch_bounds__(256) attend_kernel(const AttendParams p) {
 }
 
 // A wavefront's steps on their way: what a step reads is copied from memory to LDS, 16 bytes a lane, STAGES steps deep, without passing registers
-// (which leaves room for a fourth wavefront per SIMD) and with few, whole-line requests.  A step's place: the keys' codes of its two
+// and with few, whole-line requests (64 ragged sequences to 8192, 2 bits: 83 -> 77 us).  (Not for attend_kernel: with 32 rows the unpacking and
+// the chain of a part decide, 16 sequences of 6 tokens to 4100, 8 bits, 33.2 us as it is | 35.8 so.)  A step's place: the keys' codes of its two
 // halves, the values', then the scales and zero-points of the keys' and of the values' halves.  A row's 16-byte pieces are kept in an order that
 // goes round with the row, so that lanes reading one piece of many rows meet different banks.
 template <int BITS, int NG>
@@ -709,7 +715,7 @@ __global__ void __launch_bounds__(256) attend_few_kernel(const AttendParams p) {
     constexpr int ROW = kD * BITS / 8, MROW = 4 * NG;     // bytes of a token's codes, and of its scales and zero-points
     typedef Stage<BITS, NG> St;
     constexpr int S = St::STAGES;
-    // The wavefronts' steps; in the end their sums, in the same place (40 KB for 4 bits in groups of 32: four workgroups a compute unit).
+    // The wavefronts' steps; in the end their sums, in the same place (40 KB for 4 bits in groups of 32; three workgroups a compute unit, by their registers).
     constexpr int STEPS = kWaves * S * St::BYTES, SUMS = kWaves * R * (kPitch * 4 + 8);
     __shared__ __align__(16) unsigned char lds[STEPS > SUMS ? STEPS : SUMS];
     float(*const sums)[R][kPitch] = reinterpret_cast<float(*)[R][kPitch]>(lds);
@@ -926,8 +932,9 @@ __global__ void __launch_bounds__(256) attend_few_kernel(const AttendParams p) {
 // the first four a quarter's values each, as the second product's operands in a row, the others a quarter's keys, 16 bytes more than
 // their channels a row, which keeps 16 rows on different banks.  Two places for steps: one is filled from registers, loaded a step before,
 // while the other is met; one barrier a step.  A SIMD has a wavefront of each kind, and they dequantize at different quarters of a step, so that
-// one's vector instructions run beside the other's products.  2048 new tokens over 16384, 4 query heads, 8 KV heads, 4 bits: 592 us, 870 TFLOP/s
-// (four wavefronts and 64 tokens a step, two workgroups a compute unit: 701; without the values' operands in front of the weights 622).
+// one's vector instructions run beside the other's products.  2048 new tokens over 16384, 4 query heads, 8 KV heads, 4 bits: 557 us, 924 TFLOP/s
+// (with an unpacking of more operations 592; so, but four wavefronts and 64 tokens a step, two workgroups a compute unit, 701; without the values'
+// operands in front of the weights 622).
 // Keys are rounded to fp16 here (2^-11), so this is for results of bf16, for chunks of at least kChunkRows rows and for calls that give half of the compute units a tile, which meets its
 // sequence in one part.  (us, this | the exact form, 4 query heads, 4 bits: 8 sequences of 512 new tokens to 2048, 512 tiles, 226 | 278; 4 of 512,
 // whole prompts, 256 tiles, 42 | 49; 8 of 256 new, 1024 rows, 160 | 159; in parts, 1 of 512 to 32768, 64 tiles, 598 | 539.)
