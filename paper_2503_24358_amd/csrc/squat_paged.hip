@@ -4,9 +4,11 @@
 // Bound: HBM (a token-head in bf16 moves 512 bytes of keys and values and, 4 bits, groups of 32, 160 of store), the writing kernel also the
 // vector instructions (about 9 a value), for a few tokens the launch.  Sixteen lanes hold the 128 channels of a token-head, 8 each, so that
 // every load and store instruction covers whole lines of 16-bit tokens, and a group's statistics are two to four exchanges within
-// sixteen lanes; a workgroup takes sixteen consecutive tokens of one head, whose rows lie next to each other in a page.
-// us on one MI355X, launch included: 16384 tokens of 32 heads in fp16, 2 bits, written 82 (3.9 TB/s) and read back 69 (4.6 TB/s); 32768 of 8, 4 bits, groups of 64,
-// read back alone, 25 (6.8 TB/s, some of it from the cache in front of the memory).
+// sixteen lanes; a workgroup takes 32 consecutive tokens of one head, whose rows lie next to each other in a page, all of their loads in front of
+// the work, and the workgroups take the heads in turn, so that those that run together meet whole tokens and whole pages.
+// us on one MI355X, launches included: 16384 tokens of 32 heads in fp16, 2 bits, written and read back 119 (4.9 TB/s; 148 with 16 tokens a
+// workgroup and the heads one after the other, 140 with the heads in turn alone, 142 with 32 tokens alone); 32768 of 8, 4 bits, groups of 64, read
+// back alone 25.8 (6.7 TB/s, some of it from the cache in front of the memory; 25.3 so).
 #include "squat_paged.h"
 #include "squat_residual.h"
 
@@ -14,7 +16,10 @@ using namespace squat;
 
 namespace {
 
-constexpr int kTokens = 16;                               // tokens of one head per workgroup of 256 threads
+constexpr int kRound = 16;                                // tokens of one head that 256 threads hold
+constexpr int kRounds = 2;                                // and how many of these a workgroup has
+constexpr int kTokens = kRound * kRounds;
+constexpr int kBlocks = 32768;                            // of gridDim.y at most; more go round in z
 constexpr int kLane = 8;                                  // channels a lane
 
 struct PagedRows {
@@ -26,30 +31,36 @@ struct PagedRows {
     int n_heads;
     int page_shift;
     int group_shift;                                      // log2 of the channels a group
-    int first;                                            // blockIdx.z 0 is this one
+    int first;                                            // the first n_heads of blockIdx.x are this one's
 };
 
 // A lane's token: the row of its slot in an array of pages (or none), and where its channels are in a tensor of tokens.  (What the workgroup has in
 // common is worked out in scalars; pages are below 2^31.)
 struct Mine {
     int h, which, part, in_block;
+    int64_t block_at;                                     // the workgroup's first token
     bool live;                                            // a token of the call
     uint64_t row;
     bool stored;                                          // its slot is in the store
-    __device__ __forceinline__ explicit Mine(const PagedRows& p) {
-        h = static_cast<int>(blockIdx.y);
-        which = static_cast<int>(blockIdx.z) + p.first;
+    __device__ __forceinline__ Mine(const PagedRows& p, int round) {
+        const int second = static_cast<int>(blockIdx.x) >= p.n_heads ? 1 : 0;
+        h = static_cast<int>(blockIdx.x) - (second ? p.n_heads : 0);
+        which = p.first + second;
         part = static_cast<int>(threadIdx.x) & 15;
-        in_block = static_cast<int>(threadIdx.x) >> 4;
-        const int64_t first = static_cast<int64_t>(blockIdx.x) * kTokens;
-        live = in_block < p.n - first;
-        const uint64_t slot = static_cast<uint64_t>(p.slots[first + (live ? in_block : 0)]);
+        in_block = (static_cast<int>(threadIdx.x) >> 4) + kRound * round;
+        block_at = first_token();
+        live = in_block < p.n - block_at;
+        in_block = live ? in_block : 0;                   // (somewhere to read)
+        const uint64_t slot = static_cast<uint64_t>(p.slots[block_at + in_block]);
         stored = live && slot < static_cast<uint64_t>(p.n_slots);
         const uint32_t page = static_cast<uint32_t>(slot >> p.page_shift), within = static_cast<uint32_t>(slot) & ((1u << p.page_shift) - 1u);
         row = ((static_cast<uint64_t>(page) * static_cast<uint32_t>(p.n_heads) + static_cast<uint32_t>(h)) << p.page_shift) | within;
     }
+    static __device__ __forceinline__ int64_t first_token() {
+        return (static_cast<int64_t>(blockIdx.z) * kBlocks + blockIdx.y) * kTokens;
+    }
     __device__ __forceinline__ int64_t at(int64_t st, int64_t sh, int bytes) const {
-        return static_cast<int64_t>(blockIdx.x) * kTokens * st + h * sh + (static_cast<int64_t>(in_block) * st + part * bytes);
+        return block_at * st + h * sh + (static_cast<int64_t>(in_block) * st + part * bytes);
     }
 };
 
@@ -72,6 +83,12 @@ __device__ __forceinline__ float raw_min3(float a, float b, float c) {
 __device__ __forceinline__ float raw_max3(float a, float b, float c) {
     float r;
     asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
+__device__ __forceinline__ float raw_max3_of(float a, float b, float c) {      // a, |b|, |c|
+    float r;
+    asm("v_max3_f32 %0, %1, |%2|, |%3|" : "=v"(r) : "v"(a), "v"(b), "v"(c));
     return r;
 }
 
@@ -124,61 +141,69 @@ __global__ void __launch_bounds__(256) paged_write_kernel(const WriteParams p) {
     constexpr int PER = 16 / BITS;                        // codes a half word
     constexpr float TOP = static_cast<float>((1 << BITS) - 1);
     constexpr float NEAR = BITS == 8 ? 0.4998f : 0.49999f, FAR = BITS == 8 ? 256.0f : kQuantFastOffset;
-    const Mine mine(p.rows);
-    if (!mine.live) return;                               // the same for the sixteen lanes
-    const int part = mine.part, which = mine.which;
-    float x[kLane];
-    load8<DT>(p.x[which] + mine.at(p.st, p.sh, kLane * ES), x);
-    const float mn01 = raw_min(x[0], x[1]), mx01 = raw_max(x[0], x[1]);
-    float mn = raw_min3(raw_min3(mn01, x[2], x[3]), raw_min3(x[4], x[5], x[6]), x[7]);
-    float mx = raw_max3(raw_max3(mx01, x[2], x[3]), raw_max3(x[4], x[5], x[6]), x[7]);
-    float bad = 0.0f;                                     // NaN if a channel is infinite or NaN
+    if (Mine::first_token() >= p.rows.n) return;          // (the last round of blockIdx.y)
+    const Mine both[kRounds] = {Mine(p.rows, 0), Mine(p.rows, 1)};
+    if (!both[0].live) return;                            // the same for the sixteen lanes
+    const int part = both[0].part, which = both[0].which;
+    float of_both[kRounds][kLane];
 #pragma unroll
-    for (int e = 0; e < kLane; ++e) bad = fmaf(x[e], 0.0f, bad);
-    const int lanes = 1 << (p.rows.group_shift - 3);
-    mn = over_lanes(mn, lanes, raw_min);
-    mx = over_lanes(mx, lanes, raw_max);
-    bad = over_lanes(bad, lanes, [](float a, float b) { return a + b; });
-    if (!mine.stored) return;
-    const uint64_t row = mine.row;
-    // (max - min) / (2^b - 1), rounded to fp32: the difference as two numbers, the quotient from its remainder
-    const float range = mx - mn, rest = (mx - (range + mn)) + ((range + mn) - range - mn);
-    constexpr float RT = 1.0f / TOP;
-    const float q0 = range * RT, step = fmaf(fmaf(-q0, TOP, range) + rest, RT, q0);
-    uint16_t sbits, zbits;
-    const float s = round_f16(step + bad, sbits), z = round_f16(mn + bad, zbits);
-    const bool live = s > 0.0f;
-    const float sp = live ? s : 1.0f;
-    float inv = __builtin_amdgcn_rcpf(sp);
-    inv = fmaf(fmaf(-sp, inv, 1.0f), inv, inv);
-    const float offset = -z * inv;
-    float away = s >= 6.2e-5f && fabsf(offset) <= FAR ? 0.0f : 1.0f;          // from the nearest whole number, at most
-    Codes<BITS> c;
+    for (int k = 0; k < kRounds; ++k) load8<DT>(p.x[which] + both[k].at(p.st, p.sh, kLane * ES), of_both[k]);
 #pragma unroll
-    for (int q = 0; q < BITS / 2; ++q) {
-        float all = 0.0f;                                 // below 2^16: exact
-#pragma unroll
-        for (int e = PER - 1; e >= 0; --e) {
-            const float u = fmaf(x[PER * q + e], inv, offset), r = __builtin_rintf(u);
-            away = raw_max(away, fabsf(u - r));
-            all = fmaf(all, static_cast<float>(1 << BITS), r);
-        }
-        c.half[q] = live ? static_cast<uint32_t>(all) : 0u;
-    }
-    if (__ballot(live && away > NEAR)) {                  // (a branch for the wavefront: half of the instructions are here)
+    for (int k = 0; k < kRounds; ++k) {
+        const Mine& mine = both[k];
+        const float(&x)[kLane] = of_both[k];
+        const float mn01 = raw_min(x[0], x[1]), mx01 = raw_max(x[0], x[1]);
+        float mn = raw_min3(raw_min3(mn01, x[2], x[3]), raw_min3(x[4], x[5], x[6]), x[7]);
+        float mx = raw_max3(raw_max3(mx01, x[2], x[3]), raw_max3(x[4], x[5], x[6]), x[7]);
+        const int lanes = 1 << (p.rows.group_shift - 3);
+        mn = over_lanes(mn, lanes, raw_min);
+        mx = over_lanes(mx, lanes, raw_max);
+        // (max - min) / (2^b - 1), rounded to fp32: the difference as two numbers, the quotient from its remainder
+        const float range = mx - mn, rest = (mx - (range + mn)) + ((range + mn) - range - mn);
+        constexpr float RT = 1.0f / TOP;
+        const float q0 = range * RT, step = fmaf(fmaf(-q0, TOP, range) + rest, RT, q0);
+        uint16_t sbits, zbits;
+        const float s = round_f16(step, sbits), z = round_f16(mn, zbits);
+        const bool live = s > 0.0f;
+        const float sp = live ? s : 1.0f;
+        float inv = __builtin_amdgcn_rcpf(sp);
+        inv = fmaf(fmaf(-sp, inv, 1.0f), inv, inv);
+        const float offset = -z * inv;
+        float away = s >= 6.2e-5f && fabsf(offset) <= FAR ? 0.0f : 1.0f;          // from the nearest whole number, at most
+        float bad = 0.0f;                                 // NaN if a channel is infinite or NaN: then its quotient is, and what it enters
+        Codes<BITS> c;
 #pragma unroll
         for (int q = 0; q < BITS / 2; ++q) {
-            uint32_t half = 0u;
+            float all = 0.0f;                             // below 2^16: exact
 #pragma unroll
-            for (int e = 0; e < PER; ++e) {
-                const double r = rint((static_cast<double>(x[PER * q + e]) - static_cast<double>(z)) / static_cast<double>(sp));
-                half |= static_cast<uint32_t>(fmin(fmax(r, 0.0), static_cast<double>(TOP))) << (BITS * e);
+            for (int e = PER - 1; e > 0; e -= 2) {
+                const float u1 = fmaf(x[PER * q + e], inv, offset), r1 = __builtin_rintf(u1);
+                const float u0 = fmaf(x[PER * q + e - 1], inv, offset), r0 = __builtin_rintf(u0);
+                away = raw_max3_of(away, u1 - r1, u0 - r0);
+                all = e == PER - 1 ? r1 : fmaf(all, static_cast<float>(1 << BITS), r1);
+                all = fmaf(all, static_cast<float>(1 << BITS), r0);
             }
-            if (live && away > NEAR) c.half[q] = half;
+            bad = fmaf(all, 0.0f, bad);
+            c.half[q] = live ? static_cast<uint32_t>(all) : 0u;
         }
+        bad = over_lanes(bad, lanes, [](float a, float b) { return a + b; });
+        if (!mine.stored) continue;
+        const uint64_t row = mine.row;
+        if (__ballot(live && away > NEAR)) {              // (a branch for the wavefront: half of the instructions are here)
+#pragma unroll
+            for (int q = 0; q < BITS / 2; ++q) {
+                uint32_t half = 0u;
+#pragma unroll
+                for (int e = 0; e < PER; ++e) {
+                    const double r = rint((static_cast<double>(x[PER * q + e]) - static_cast<double>(z)) / static_cast<double>(sp));
+                    half |= static_cast<uint32_t>(fmin(fmax(r, 0.0), static_cast<double>(TOP))) << (BITS * e);
+                }
+                if (live && away > NEAR) c.half[q] = half;
+            }
+        }
+        c.store(p.rows.codes[which] + row * (kD * BITS / 32), part);
+        if ((part & (lanes - 1)) == 0) p.rows.meta[which][meta_at(p.rows, row, part)] = bad == 0.0f ? sbits | (static_cast<uint32_t>(zbits) << 16) : 0x7E007E00u;
     }
-    c.store(p.rows.codes[which] + row * (kD * BITS / 32), part);
-    if ((part & (lanes - 1)) == 0) p.rows.meta[which][meta_at(p.rows, row, part)] = sbits | (static_cast<uint32_t>(zbits) << 16);
 }
 
 // Rows that squat_quantize_keys' kernel wrote densely, [heads, n, ...], to their slots.
@@ -190,16 +215,20 @@ struct DealParams {
 
 template <int BITS>
 __global__ void __launch_bounds__(256) paged_deal_kernel(const DealParams p) {
-    const Mine mine(p.rows);
-    if (!mine.stored) return;
-    const int part = mine.part;
-    const uint64_t row = mine.row;
-    const int64_t from = mine.h * p.rows.n + static_cast<int64_t>(blockIdx.x) * kTokens + mine.in_block;
-    Codes<BITS> c;
-    c.load(p.codes + from * (kD * BITS / 32), part);
-    c.store(p.rows.codes[0] + row * (kD * BITS / 32), part);
-    const int ng = kD >> p.rows.group_shift;
-    if (part < ng) p.rows.meta[0][row * ng + part] = p.scale[from * ng + part] | (static_cast<uint32_t>(p.zero[from * ng + part]) << 16);
+    if (Mine::first_token() >= p.rows.n) return;
+#pragma unroll
+    for (int k = 0; k < kRounds; ++k) {
+        const Mine mine(p.rows, k);
+        if (!mine.stored) continue;
+        const int part = mine.part;
+        const uint64_t row = mine.row;
+        const int64_t from = mine.h * p.rows.n + mine.block_at + mine.in_block;
+        Codes<BITS> c;
+        c.load(p.codes + from * (kD * BITS / 32), part);
+        c.store(p.rows.codes[0] + row * (kD * BITS / 32), part);
+        const int ng = kD >> p.rows.group_shift;
+        if (part < ng) p.rows.meta[0][row * ng + part] = p.scale[from * ng + part] | (static_cast<uint32_t>(p.zero[from * ng + part]) << 16);
+    }
 }
 
 struct ReadParams {
@@ -234,24 +263,30 @@ template <int BITS, int DT>
 __global__ void __launch_bounds__(256) paged_read_kernel(const ReadParams p) {
     constexpr int ES = DT == SQUAT_F32 ? 4 : 2;
     constexpr int PER = 16 / BITS;
-    const Mine mine(p.rows);
-    if (!mine.live) return;
-    const int part = mine.part, which = mine.which;
-    const uint64_t row = mine.row;
-    float x[kLane];
-    if (!mine.stored) {
+    if (Mine::first_token() >= p.rows.n) return;          // (the last round of blockIdx.y)
+    const Mine both[kRounds] = {Mine(p.rows, 0), Mine(p.rows, 1)};
+    if (!both[0].live) return;
+    const int part = both[0].part, which = both[0].which;
+    Codes<BITS> c[kRounds];
+    uint32_t meta[kRounds];
 #pragma unroll
-        for (int e = 0; e < kLane; ++e) x[e] = 0.0f;
-    } else {
-        Codes<BITS> c;
-        c.load(p.rows.codes[which] + row * (kD * BITS / 32), part);
-        const uint32_t m = p.rows.meta[which][meta_at(p.rows, row, part)];
-        const float s = static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(m & 0xFFFFu)));
-        const float z = static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(m >> 16)));
-#pragma unroll
-        for (int e = 0; e < kLane; ++e) x[e] = fmaf(static_cast<float>((c.half[e / PER] >> (e % PER * BITS)) & ((1u << BITS) - 1u)), s, z);
+    for (int k = 0; k < kRounds; ++k) {
+        const uint64_t row = both[k].stored ? both[k].row : 0;                // (somewhere to read: a store has a page)
+        c[k].load(p.rows.codes[which] + row * (kD * BITS / 32), part);
+        meta[k] = p.rows.meta[which][meta_at(p.rows, row, part)];
     }
-    store8<DT>(p.x[which] + mine.at(p.st, p.sh, kLane * ES), x);
+#pragma unroll
+    for (int k = 0; k < kRounds; ++k) {
+        const float s = static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(meta[k] & 0xFFFFu)));
+        const float z = static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(meta[k] >> 16)));
+        float x[kLane];
+#pragma unroll
+        for (int e = 0; e < kLane; ++e) {
+            const float code = static_cast<float>((c[k].half[e / PER] >> (e % PER * BITS)) & ((1u << BITS) - 1u));
+            x[e] = both[k].stored ? fmaf(code, s, z) : 0.0f;
+        }
+        if (both[k].live) store8<DT>(p.x[which] + both[k].at(p.st, p.sh, kLane * ES), x);
+    }
 }
 
 int page_shift(int page_tokens) {
@@ -276,10 +311,18 @@ PagedRows rows_of(const squat_paged_store* s, const int64_t* slots, int64_t n) {
     return r;
 }
 
+// A workgroup for every head of `arrays` (keys, values or both) and run of tokens, the heads in turn: what runs together reads whole tokens and
+// writes whole pages, or the other way round.
+dim3 grid_of(const squat_paged_store* s, int64_t n, int arrays) {
+    const int64_t blocks = (n + kTokens - 1) / kTokens;
+    return dim3(static_cast<unsigned>(s->n_kv_heads * arrays), static_cast<unsigned>(blocks < kBlocks ? blocks : kBlocks),
+                static_cast<unsigned>((blocks + kBlocks - 1) / kBlocks));
+}
+
 // What both directions ask of the tokens' tensors.
 int check_tokens(const squat_paged_store* s, squat_dtype dt, int64_t n, int64_t st, int64_t sh) {
     if (elem_size(dt) == 0) return SQUAT_E_BADDTYPE;
-    if (n < 0 || (n + kTokens - 1) / kTokens > 0x7FFFFFFF) return SQUAT_E_BADSHAPE;
+    if (n < 0 || (n + kTokens - 1) / kTokens > static_cast<int64_t>(kBlocks) * 65535) return SQUAT_E_BADSHAPE;
     if (st < kD || (sh < kD && s->n_kv_heads > 1) || sh < 0) return SQUAT_E_BADSHAPE;
     if ((st % 8) || (sh % 8)) return SQUAT_E_ALIGN;
     return SQUAT_OK;
@@ -332,7 +375,7 @@ extern "C" int squat_paged_write(const squat_paged_store* store, const void* k, 
     p.x[1] = static_cast<const unsigned char*>(v);
     p.st = stride_token * es;
     p.sh = stride_head * es;
-    dim3 grid(static_cast<unsigned>((n_tokens + kTokens - 1) / kTokens), static_cast<unsigned>(store->n_kv_heads), 2);
+    dim3 grid = grid_of(store, n_tokens, 2);
     if (update) {
         // the keys: densely into the workspace, then to their slots
         const size_t need = squat_paged_write_workspace(store, n_tokens, 1);
@@ -352,7 +395,7 @@ extern "C" int squat_paged_write(const squat_paged_store* store, const void* k, 
         rc = quantize_keys_into(k, dt, 1, store->n_kv_heads, n_tokens, kD, 0, stride_head, stride_token, update, 0, store->bits,
                                 store->group, g, codes, scale, zero, n_tokens, 0, stream);
         if (rc) return rc;
-        grid.z = 1;
+        grid = grid_of(store, n_tokens, 1);
         if (store->bits == 2) hipLaunchKernelGGL((paged_deal_kernel<2>), grid, dim3(256), 0, s, d);
         else hipLaunchKernelGGL((paged_deal_kernel<4>), grid, dim3(256), 0, s, d);
         rc = check_launch();
@@ -384,8 +427,7 @@ extern "C" int squat_paged_read(const squat_paged_store* store, const int64_t* s
     p.x[1] = static_cast<unsigned char*>(v_out);
     p.st = stride_token * es;
     p.sh = stride_head * es;
-    const dim3 grid(static_cast<unsigned>((n_tokens + kTokens - 1) / kTokens), static_cast<unsigned>(store->n_kv_heads),
-                    k_out && v_out ? 2 : 1);
+    const dim3 grid = grid_of(store, n_tokens, k_out && v_out ? 2 : 1);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     switch (store->bits) {
         case 2: launch_read<2>(out_dt, grid, s, p); break;

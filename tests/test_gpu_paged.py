@@ -226,3 +226,54 @@ def test_slots_past_four_gigabytes():
     same = small.attention(q, torch.tensor([[0, 1], [2, 3]], dtype=torch.int32).cuda(), torch.tensor([300, 512], dtype=torch.int32).cuda(),
                            torch.tensor([0, 1, 2], dtype=torch.int32).cuda(), 0.1)
     assert torch.equal(out, same)
+
+
+@pytest.mark.parametrize("n", [15, 16, 17, 31, 32, 48, 49, 63, 64, 65])
+@pytest.mark.parametrize("update", [False, True])
+def test_counts_around_a_workgroup(n, update):
+    """Workgroups whose tokens end anywhere; with an update matrix the keys take another path to their slots."""
+    gen = torch.Generator().manual_seed(n)
+    k, v = (torch.randn(n, 3, 128, generator=gen).half().cuda() for _ in range(2))
+    slots = torch.randperm(96, generator=gen)[:n]
+    slots[n // 2] = -1
+    s = _store(6, 3, 16, 4, 32, fill=-1)
+    keep = slots >= 0
+    here = keep.cuda()
+    if update:
+        u = torch.randn(3, 128, 128, generator=gen).cuda() / 64
+        s.write(k, v, slots.cuda(), update=u, g=32)
+        codes, scale, zero = squat.quantize_keys(k.transpose(0, 1).unsqueeze(0), u, 4, 32, 32)
+        kc, km, vc, vm = _rows(s, slots[keep].numpy(), 16)
+        assert np.array_equal(kc, _host(codes)[0].transpose(1, 0, 2)[keep])
+        assert np.array_equal(km, np.stack([_host(scale)[0].transpose(1, 0, 2), _host(zero)[0].transpose(1, 0, 2)], -1)[keep])
+        want_c, want_m = P.quantize(v[here].double().cpu().numpy(), 4, 32)
+        assert np.array_equal(P.unpack(vc, 4), want_c) and np.array_equal(vm, want_m)
+    else:
+        s.write(k, v, slots.cuda())
+        _check(k[here], v[here], s, slots[keep].numpy(), 16, 4, 32)
+    free = np.setdiff1d(np.arange(96), slots.numpy())
+    assert all((a == -1).all() for a in _rows(s, free, 16)[::2])
+    kr, vr = s.read(slots.cuda(), torch.float32)
+    assert (kr[n // 2] == 0).all() and (vr[n // 2] == 0).all()
+    kc, km, vc, vm = _rows(s, slots[keep].numpy(), 16)
+    _read_ok(kr[here], kc, km, 4)
+    _read_ok(vr[here], vc, vm, 4)
+
+
+def test_more_tokens_than_a_dimension_of_workgroups():
+    """2^20 tokens and some: one call does what two calls do."""
+    n, page = (1 << 20) + 77, 256
+    pages = -(-n // page)
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    k, v = (torch.randn(n, 1, 128, generator=gen, device="cuda").bfloat16() for _ in range(2))
+    slots = torch.randperm(pages * page, generator=gen, device="cuda")[:n]
+    one, two = (_store(pages, 1, page, 2, 128) for _ in range(2))
+    one.write(k, v, slots)
+    for at in (slice(0, 1 << 19), slice(1 << 19, n)):
+        two.write(k[at], v[at], slots[at])
+    for a, b in zip(one.arrays[:4], two.arrays[:4]):
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+    got = one.read(slots)
+    for at in (slice(0, 1 << 19), slice(1 << 19, n)):
+        for x, y in zip(got, two.read(slots[at])):
+            assert torch.equal(x[at], y)
