@@ -30,11 +30,13 @@ constexpr int kStep = 32;                                 // tokens per step of 
 constexpr int kWaves = 4;
 constexpr float kLift = 11.0f, kSlack = 4.0f;
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
-// A launch's workgroups per compute unit, where there is work for them: as many as it holds at once (three of a few rows, two of more), which
-// suits sequences that end together, and for the few rows of many sequences, whose lengths differ, more; and a part's steps at least.
-// us, 1 sequence of 131072 tokens, 8 query heads, 3 | 4 | 6 a compute unit 39.0 | 42.0 | 45.1; 64 ragged ones to 8192, 4 query heads, 6 | 8 | 12
-// 80.0 | 77.3 | 76.8; 16 of 6 tokens each to 4100, 8 bits, 2 | 4 | 8 36.4 | 40.1 | 44.4 (more rows, more sums to put together).
-constexpr int kTargetOne = 3, kTargetMany = 8, kTargetRows = 2, kLeast = 8;
+// A launch's workgroups per compute unit, where there is work for them, and a part's steps at least: as many as it holds at once, which is two for
+// 8 bits (their steps' LDS) and for more than a few rows (registers), else three, which suits sequences that end together; one more for
+// several sequences, whose lengths differ.
+// us, a few rows, 8 bits, 2 | 3 | 8 a compute unit: 64 sequences of 4608 tokens 115 | 123 | 130, ragged ones 75 | 84 | 80, one of 131072 54 | 60 | 59.
+// 2 bits, 3 | 4 | 8: 64 of 4608 60 | 59 | 61, ragged 48 | 47 | 46 (to 8192 76 | 77 | 73); 4 bits: 16 of 8192 35 | 36 | 40, ragged 31 | 27 | 31; one of
+// 131072, 8 query heads, 39 | 42 | 45 (6).  More rows, 8 bits, 16 of 6 tokens to 4100, 2 | 3 | 4: 33 | 34 | 36.
+constexpr int kTargetTwo = 2, kTargetOne = 3, kTargetMany = 4, kLeast = 8;
 constexpr int kPitch = kD + 4;                            // floats per row of a wavefront's sums in LDS
 
 struct AttendParams {
@@ -1358,7 +1360,8 @@ Plan plan_attend(const squat_paged_store* s, squat_dtype dt, int n_seqs, int64_t
     tile(kChunkTile);
     a.chunk = dt == SQUAT_BF16 && max_new * q_per_kv >= kChunkRows && busy >= device_cu_count() / 2;
     if (!a.chunk) tile(a.nq == 0 ? few : 16 * a.nq);
-    const int64_t steps = (max_kv + kStep - 1) / kStep, wanted = a.chunk ? 1 : ((a.nq > 0 ? kTargetRows : n_seqs < 4 ? kTargetOne : kTargetMany) * device_cu_count() + busy - 1) / busy;
+    const int target = a.nq > 0 || s->bits == 8 ? kTargetTwo : n_seqs < 4 ? kTargetOne : kTargetMany;
+    const int64_t steps = (max_kv + kStep - 1) / kStep, wanted = a.chunk ? 1 : (target * device_cu_count() + busy - 1) / busy;
     int64_t span = (steps + wanted - 1) / wanted;
     span = span < kLeast ? kLeast : span;
     int64_t n = (steps + span - 1) / span;
