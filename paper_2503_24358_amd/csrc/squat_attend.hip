@@ -16,7 +16,7 @@
 // The running maximum m of a row is raised only when a logit passes it by more than 2^kSlack (the rows' sums are rescaled then, for
 // all of them): p = 2^(x - m + kLift), at most 2^15, and small weights keep their bits down to 2^-(24 + kLift) of the largest.
 //
-// us on one MI355X, launch included (bf16, 8 KV heads): a decoded token of 64 sequences to 8192 tokens, 2 bits, 71.7 (3.2 TB/s of store); one of
+// us on one MI355X, launch included (bf16, 8 KV heads): a decoded token of 64 ragged sequences to 8192 tokens, 2 bits, 77 (3.0 TB/s of store); of 4608 each, 8 bits, 115 (5.5 TB/s); one of
 // 131072, 4 bits, 38 (4.0 TB/s); 6 tokens of each of 16 to 4100, 8 bits, 33 (2.7 TB/s); 2048 over 16384, 4 bits, 557 (924 TFLOP/s).
 #include <type_traits>
 
@@ -937,10 +937,12 @@ __global__ void __launch_bounds__(256) attend_few_kernel(const AttendParams p) {
 // one's vector instructions run beside the other's products.  2048 new tokens over 16384, 4 query heads, 8 KV heads, 4 bits: 557 us, 924 TFLOP/s
 // (with an unpacking of more operations 592; so, but four wavefronts and 64 tokens a step, two workgroups a compute unit, 701; without the values'
 // operands in front of the weights 622).
-// Keys are rounded to fp16 here (2^-11), so this is for results of bf16, for chunks of at least kChunkRows rows and for calls that give half of the compute units a tile, which meets its
-// sequence in one part.  (us, this | the exact form, 4 query heads, 4 bits: 8 sequences of 512 new tokens to 2048, 512 tiles, 226 | 278; 4 of 512,
-// whole prompts, 256 tiles, 42 | 49; 8 of 256 new, 1024 rows, 160 | 159; in parts, 1 of 512 to 32768, 64 tiles, 598 | 539.)
-constexpr int kChunkRows = 2048, kChunkTile = 256, kChunkStep = 128, kChunkWaves = 8, kKeyPitch = 2 * kD + 16;
+// Keys are rounded to fp16 here (2^-11), so this is for results of bf16.  A tile meets its sequence in one part, so it is for calls with tiles
+// enough, and the more rows a sequence has the fewer: from kChunkLeast rows on where rows times tiles (with work, over all heads) are kChunkRows times
+// half of the compute units.  us, this | the exact form, rows x tiles: 4096 x 256 42 | 49; 2048 x 512 226 | 278; 1909 x 256 83 | 97; 1610 x 224 78 | 85;
+// 1000 x 512 63 | 85; 735 x 660 170 | 200; 528 x 1170 74 | 91; but 1258 x 160 74 | 71; 1015 x 160 49 | 40; 991 x 128 144 | 120; in parts, 2048 x 64,
+// 598 | 539.
+constexpr int kChunkRows = 2048, kChunkLeast = 512, kChunkTile = 256, kChunkStep = 128, kChunkWaves = 8, kKeyPitch = 2 * kD + 16;
 
 // Which channel element e of a key's unit of 8 is (see code_pair: a word's halves are unpacked together).
 template <int BITS>
@@ -1358,7 +1360,7 @@ Plan plan_attend(const squat_paged_store* s, squat_dtype dt, int n_seqs, int64_t
         busy = (busy < a.tiles ? busy : a.tiles) * s->n_kv_heads;
     };
     tile(kChunkTile);
-    a.chunk = dt == SQUAT_BF16 && max_new * q_per_kv >= kChunkRows && busy >= device_cu_count() / 2;
+    a.chunk = dt == SQUAT_BF16 && max_new * q_per_kv >= kChunkLeast && max_new * q_per_kv * busy >= static_cast<int64_t>(kChunkRows) * (device_cu_count() / 2);
     if (!a.chunk) tile(a.nq == 0 ? few : 16 * a.nq);
     const int target = a.nq > 0 || s->bits == 8 ? kTargetTwo : n_seqs < 4 ? kTargetOne : kTargetMany;
     const int64_t steps = (max_kv + kStep - 1) / kStep, wanted = a.chunk ? 1 : (target * device_cu_count() + busy - 1) / busy;

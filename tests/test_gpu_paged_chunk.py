@@ -1,4 +1,4 @@
-"""squat_paged_attention with many rows of bf16 queries (2048 a sequence, and 128 tiles of 256 rows over the KV heads), which meet dequantized keys and values: against the definition in 64 bits.  Keys are rounded
+"""squat_paged_attention with many rows of bf16 queries (from 512 a sequence on, where there are tiles enough), which meet dequantized keys and values: against the definition in 64 bits.  Keys are rounded
 to fp16 there, so a logit's bound has 2^-11 of its products beside what test_gpu_paged_attention counts."""
 import numpy as np
 import pytest
@@ -36,6 +36,13 @@ def test_ragged_chunks():
     """Whole prompts, a chunk behind a long beginning, a decoded token and a sequence without tokens in one call; lengths that end inside a step."""
     _run(50, [521, 1337, 90, 0, 31], [521, 77, 1, 0, 31], 10, 4, 4, 32, 64)
     _run(51, [515, 1, 65], [515, 1, 40], 12, 4, 2, 64, 16)
+
+
+@pytest.mark.parametrize("bits, group", [(2, 128), (4, 32), (8, 64)])
+def test_many_short_chunks(bits, group):
+    """528 rows a sequence, and as many tiles as that takes; lengths from the chunk's own on."""
+    _run(57, [33, 34, 47, 64, 65, 95, 128, 129, 160, 200, 256, 257], [33] * 12, 14, 16, bits, group, 16)
+    _run(58, [90, 33, 400, 5, 0, 70, 33, 60, 80, 41, 129, 222, 301], [33, 33, 33, 5, 0, 33, 33, 33, 33, 33, 33, 33, 33], 14, 16, bits, group, 32)
 
 
 def test_rows_that_see_nothing():
