@@ -16,8 +16,9 @@
 // The running maximum m of a row is raised only when a logit passes it by more than 2^kSlack (the rows' sums are rescaled then, for
 // all of them): p = 2^(x - m + kLift), at most 2^15, and small weights keep their bits down to 2^-(24 + kLift) of the largest.
 //
-// us on one MI355X, launch included (bf16, 8 KV heads): a decoded token of 64 ragged sequences to 8192 tokens, 2 bits, 77 (3.0 TB/s of store); of 4608 each, 8 bits, 115 (5.5 TB/s); one of
-// 131072, 4 bits, 38 (4.0 TB/s); 6 tokens of each of 16 to 4100, 8 bits, 33 (2.7 TB/s); 2048 over 16384, 4 bits, 557 (924 TFLOP/s).
+// us on one MI355X, launch included (bf16, 8 KV heads): a decoded token of 64 ragged sequences to 8192 tokens, 2 bits, 77 (3.0 TB/s of store); of
+// 64 of 4608 each, 8 bits, 115 (5.5 TB/s); of one of 131072, 4 bits, 38 (4.0 TB/s); 6 tokens of each of 16 to 4100, 8 bits, 33 (2.7 TB/s); 2048
+// over 16384, 4 bits, 557 (924 TFLOP/s).
 #include <type_traits>
 
 #include "squat_paged.h"
@@ -681,8 +682,8 @@ struct Stage {
         } else {
             copy(first + code_off[0], to);
             copy(first + code_off[1], to + 1024);
-            copy(second + code_off[0], to + 2048);
-            copy(second + code_off[1], to + 3072);
+            copy(second + code_off[0], to + 2 * 1024);
+            copy(second + code_off[1], to + 3 * 1024);
         }
     }
     __device__ __forceinline__ void fetch(const AttendParams& p, const Place& a, unsigned char* to) const {
